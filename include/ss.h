@@ -62,6 +62,10 @@ extern "C" {
 #define SS_F32 0
 #define SS_BF16 1
 
+/* element formats of a cache in microscaling blocks (n5) */
+#define SS_KV_MXFP8 0 /* e4m3, 8 bits */
+#define SS_KV_MXFP4 1 /* e2m1, 4 bits */
+
 /* limits */
 #define SS_MAX_T 64     /* tree nodes per sequence (ancestor sets are 64-bit) */
 #define SS_MAX_GAMMA 8  /* speculative streams per node                       */
@@ -662,6 +666,82 @@ int ss_kv_alloc_pages(int32_t* block_table, int max_pages_per_seq, const int32_t
                       const int32_t* n_accept, int B, int page_size, int max_depth,
                       const int32_t* free_pages, int32_t* free_count, int32_t* n_commit,
                       void* stream);
+
+/*
+ * n5. The key/value cache in microscaling formats: the cache of n3 in 8 or 4 bits
+ * per value.  Of every cached (token, KV head) the D features are D/32 blocks of
+ * 32; a block is 32 elements e and one scale byte s, and stands for the values
+ *    e * 2^(s-127)
+ * format SS_KV_MXFP8: elements e4m3 (largest 448), one byte each; SS_KV_MXFP4:
+ * elements e2m1 (0, .5, 1, 1.5, 2, 3, 4, 6 and their negatives), two per byte, the
+ * even feature in the low half.  Rows are token-major for keys AND values:
+ *  k_cache, v_cache [num_pages,Hkv,page_size,D or D/2] bytes (16-byte aligned)
+ *  k_scale, v_scale [num_pages,Hkv,page_size,D/32]     bytes (4-byte aligned)
+ * Quantisation of a block: s is the smallest number in [0,254] with which no
+ * element lies beyond the format's largest, so none is clamped; elements are
+ * rounded to nearest, ties to the even code, and keep the sign of a zero.  A value
+ * is then off by at most half an element's step.  A block that holds a NaN or an
+ * infinity gets s = 255 and zeros as elements, and reads as NaN.
+ * Limits (all calls): D in {64,128}, page_size in {16,32,64}, B <= 65535.
+ * Page ids are clamped and positions at or past max_pages_per_seq*page_size
+ * dropped as in ss_kv_commit.  Pages that are written must not be shared.
+ *
+ * ss_kv_append_mx: row j < n_rows[b] of k_rows, v_rows [B,S,Hkv,D] (dtype SS_F32 or
+ *  SS_BF16, 16-byte aligned) is quantised to position seq_lens[b] + j: a prompt, or
+ *  the next chunk of one.  n_rows [B] is clamped to [0,S]; rows at and past it are
+ *  not read.  new_seq_lens [B] out, or NULL: seq_lens[b] + number of rows written.
+ *  Must not be the seq_lens array itself.
+ *
+ * ss_kv_commit_mx: ss_kv_commit for this cache; the rows of the accepted path are
+ *  quantised as they are written.
+ *
+ * ss_kv_read_mx: row j of k_rows, v_rows [B,S,Hkv,D] (dtype as above) gets the
+ *  values that position first[b] + j holds, for positions below seq_lens[b]; rows
+ *  behind those are left as they are.  first [B] or NULL (0 for all); negative
+ *  entries count as 0.  Values are exact in fp32, and in bf16 but for parts of an
+ *  e4m3 value below 2^-133 (rounded to nearest even).
+ */
+int ss_kv_append_mx(const void* k_rows, const void* v_rows, void* k_cache, void* k_scale, void* v_cache,
+                    void* v_scale, const int32_t* block_table, int max_pages_per_seq, int num_pages,
+                    const int32_t* seq_lens, const int32_t* n_rows, int B, int S, int Hkv, int D,
+                    int page_size, int dtype, int format, int32_t* new_seq_lens, void* stream);
+int ss_kv_commit_mx(const void* k_new, const void* v_new, void* k_cache, void* k_scale, void* v_cache,
+                    void* v_scale, const int32_t* block_table, int max_pages_per_seq, int num_pages,
+                    const int32_t* seq_lens, const int32_t* path, const int32_t* n_accept, int B, int T,
+                    int gamma, int Hkv, int D, int page_size, int max_depth, int dtype, int format,
+                    int32_t* new_seq_lens, void* stream);
+int ss_kv_read_mx(const void* k_cache, const void* k_scale, const void* v_cache, const void* v_scale,
+                  const int32_t* block_table, int max_pages_per_seq, int num_pages, const int32_t* first,
+                  const int32_t* seq_lens, int B, int S, int Hkv, int D, int page_size, int dtype,
+                  int format, void* k_rows, void* v_rows, void* stream);
+
+/*
+ * n5, a2 over that cache: ss_msa_attention (n_nodes NULL) or ss_msa_attention_pruned
+ * (n_nodes [B]) with the cached keys and values in a microscaling format.  The step's
+ * own rows k_new, v_new are attended to as they are given; q, k_new, v_new and out are
+ * SS_BF16 (16-byte aligned).  Scores use the queries without further rounding but for
+ * parts of a query below 2^-22 of its largest feature; sums, softmax and accumulation
+ * are fp32, and the probabilities are rounded to bf16 as in a2.  One kernel.
+ * Limits: those of a2 and n5; flags: SS_STREAM_EXCLUDE_SELF only.
+ * A sequence is cut into splits of equal length, chosen from its own length and
+ * ss_msa_mx_plan's number of splits; no other sequence changes its result.
+ * workspace: at least ss_msa_mx_workspace_bytes(...) bytes with max_seq_len =
+ * max_pages_per_seq*page_size (not used if the plan has one split).  Its front holds
+ * counters, under the rules of a2: zeros before the first call
+ * (ss_msa_workspace_init), zeros after every call, not shared by calls that may run at
+ * the same time.  One workspace can serve this call and a2 in turn.
+ * ss_msa_mx_plan: most splits a sequence has in a call of this shape and query rows per
+ * workgroup; either pointer may be NULL.  Host-only.
+ */
+size_t ss_msa_mx_workspace_bytes(int B, int T, int gamma, int H, int Hkv, int D, int max_seq_len);
+int ss_msa_mx_plan(int B, int T, int gamma, int H, int Hkv, int D, int max_seq_len, int* n_splits,
+                   int* rows_per_workgroup);
+int ss_msa_attention_mx(const void* q, const void* k_new, const void* v_new, const void* k_cache,
+                        const void* k_scale, const void* v_cache, const void* v_scale,
+                        const int32_t* block_table, int max_pages_per_seq, int num_pages,
+                        const int32_t* seq_lens, const int32_t* parent, const int32_t* n_nodes, int B,
+                        int T, int gamma, int H, int Hkv, int D, int page_size, float scale, int format,
+                        uint32_t flags, void* out, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -343,3 +343,30 @@ def lm_head_topk_live(hidden, W, K: int, rows, want_logits: bool = False):
         if want_logits:
             z[rows] = r[2]
     return (idx, val, z) if want_logits else (idx, val)
+
+
+MXFP8, MXFP4 = 0, 1
+
+
+def mx_quantise(x, fmt: int):
+    """n5.  x [...,D] float32 -> (element bytes [...,D] or packed [...,D/2], the even feature in the low half; scale bytes
+    [...,D/32])."""
+    x = _f32(x)
+    assert x.shape[-1] % 32 == 0
+    code = np.zeros(x.shape, np.uint8)
+    scale = np.zeros(x.shape[:-1] + (x.shape[-1] // 32,), np.uint8)
+    _load().ora_mx_quantise(_p(x), ctypes.c_long(x.size // 32), fmt, _p(code), _p(scale))
+    if fmt == MXFP4:
+        code = (code[..., 0::2] | (code[..., 1::2] << 4)).astype(np.uint8)
+    return code, scale
+
+
+def mx_values(code, scale, fmt: int):
+    """n5.  The float64 values [...,D] that element and scale bytes stand for."""
+    code, scale = np.ascontiguousarray(code, np.uint8), np.ascontiguousarray(scale, np.uint8)
+    if fmt == MXFP4:
+        code = np.ascontiguousarray(np.stack((code & 15, code >> 4), -1).reshape(code.shape[:-1] + (2 * code.shape[-1],)))
+    assert code.shape[:-1] == scale.shape[:-1] and code.shape[-1] == 32 * scale.shape[-1]
+    out = np.zeros(code.shape, np.float64)
+    _load().ora_mx_values(_p(code), _p(scale), ctypes.c_long(scale.size), fmt, _p(out))
+    return out

@@ -594,3 +594,62 @@ void ora_stream_insert_linear(const float* M, const float* fM, const float* P, c
       }
     }
 }
+
+
+/*
+ * n5, microscaling blocks: 32 elements and a power of two 2^(s-127).  fmt 0: elements e4m3 (sign, 4 exponent bits with bias 7,
+ * 3 mantissa bits; code 127 is NaN), fmt 1: e2m1 (sign, 2 exponent bits with bias 1, 1 mantissa bit).  The value of an element
+ * code, from its bits.
+ */
+static double ora_mx_element(int code, int fmt) {
+  int man_bits = fmt == 0 ? 3 : 1, exp_bits = fmt == 0 ? 4 : 2, bias = fmt == 0 ? 7 : 1;
+  int man = code & ((1 << man_bits) - 1), ex = (code >> man_bits) & ((1 << exp_bits) - 1), neg = (code >> (man_bits + exp_bits)) & 1;
+  double v;
+  if (fmt == 0 && ex == 15 && man == 7) return NAN;
+  v = ex == 0 ? ldexp((double)man, 1 - bias - man_bits) : ldexp((double)((1 << man_bits) + man), ex - bias - man_bits);
+  return neg ? -v : v;
+}
+
+/* x [n_blocks][32] -> code [n_blocks][32] (one element per byte), scale [n_blocks].  s is the smallest number in [0,254] with
+ * which the largest element of the format reaches the block's largest magnitude; elements are the nearest there are, of two as
+ * near the one with the even code.  A block with a NaN or an infinity: s = 255, all codes 0. */
+void ora_mx_quantise(const float* x, long n_blocks, int fmt, uint8_t* code, uint8_t* scale) {
+  int n_mag = fmt == 0 ? 127 : 8;
+  double top = ora_mx_element(n_mag - 1, fmt);
+  for (long b = 0; b < n_blocks; b++) {
+    const float* xb = x + b * 32;
+    uint8_t* cb = code + b * 32;
+    double amax = 0.0;
+    int bad = 0, s = 0;
+    for (int i = 0; i < 32; i++) {
+      if (isnan(xb[i]) || isinf(xb[i])) bad = 1;
+      if (fabs((double)xb[i]) > amax) amax = fabs((double)xb[i]);
+    }
+    if (bad) {
+      scale[b] = 255;
+      memset(cb, 0, 32);
+      continue;
+    }
+    while (s < 254 && amax > ldexp(top, s - 127)) s++;
+    scale[b] = (uint8_t)s;
+    for (int i = 0; i < 32; i++) {
+      double y = ldexp(fabs((double)xb[i]), 127 - s), best_d = INFINITY;
+      int best = 0;
+      for (int c = 0; c < n_mag; c++) {
+        double d = fabs(ora_mx_element(c, fmt) - y);
+        if (d < best_d || (d == best_d && c % 2 == 0)) {
+          best = c;
+          best_d = d;
+        }
+      }
+      cb[i] = (uint8_t)(best + (signbit(xb[i]) ? (fmt == 0 ? 128 : 8) : 0));
+    }
+  }
+}
+
+/* code [n_blocks][32], scale [n_blocks] -> the values they stand for. */
+void ora_mx_values(const uint8_t* code, const uint8_t* scale, long n_blocks, int fmt, double* out) {
+  for (long b = 0; b < n_blocks; b++)
+    for (int i = 0; i < 32; i++)
+      out[b * 32 + i] = scale[b] == 255 ? NAN : ldexp(ora_mx_element(code[b * 32 + i], fmt), (int)scale[b] - 127);
+}

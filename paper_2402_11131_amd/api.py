@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_PKG, "libss.so")
 
 SS_OK = 0
 SS_F32, SS_BF16 = 0, 1
+SS_KV_MXFP8, SS_KV_MXFP4 = 0, 1
 SS_STREAM_EXCLUDE_SELF = 1
 SS_MSA_PARTIALS_ONLY = 2
 SS_MSA_MERGE_ONLY = 4
@@ -31,6 +32,7 @@ EXPORTS = (
     "ss_tree_verify", "ss_tree_draft", "ss_full_tree_template_host", "ss_kv_commit", "ss_kv_alloc_pages", "ss_linear_rows", "ss_linear_rows_ws", "ss_linear_rows_workspace_bytes", "ss_linear_rows_splits", "ss_stream_insert", "ss_stream_insert_linear", "ss_stream_insert_linear_workspace_bytes", "ss_value_rotate",
     "ss_lm_head_logsumexp", "ss_transition_probs", "ss_tree_prune", "ss_live_rows", "ss_msa_attention_pruned",
     "ss_linear_rows_live", "ss_lm_head_argmax_topk_live", "ss_lm_head_verify_draft_live",
+    "ss_kv_append_mx", "ss_kv_commit_mx", "ss_kv_read_mx", "ss_msa_mx_workspace_bytes", "ss_msa_mx_plan", "ss_msa_attention_mx",
 )
 
 _lib = None
@@ -105,6 +107,13 @@ def load_library() -> ctypes.CDLL:
     lib.ss_linear_rows_live.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, vp, i32, vp]
     lib.ss_lm_head_argmax_topk_live.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, i32, vp, sz, vp]
     lib.ss_lm_head_verify_draft_live.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, i32, i32, i32, i32, vp, vp, vp, i32] + [vp] * 8 + [vp, vp, i32, vp, sz, vp]
+    lib.ss_kv_append_mx.argtypes = [vp] * 7 + [i32, i32, vp, vp] + [i32] * 7 + [vp, vp]
+    lib.ss_kv_commit_mx.argtypes = [vp] * 7 + [i32, i32, vp, vp, vp] + [i32] * 9 + [vp, vp]
+    lib.ss_kv_read_mx.argtypes = [vp] * 5 + [i32, i32, vp, vp] + [i32] * 7 + [vp, vp, vp]
+    lib.ss_msa_mx_workspace_bytes.argtypes = [i32] * 7
+    lib.ss_msa_mx_workspace_bytes.restype = sz
+    lib.ss_msa_mx_plan.argtypes = [i32] * 7 + [c.POINTER(c.c_int)] * 2
+    lib.ss_msa_attention_mx.argtypes = [vp] * 8 + [i32, i32, vp, vp, vp] + [i32] * 7 + [c.c_float, i32, u32, vp, vp, sz, vp]
     for name in EXPORTS:
         getattr(lib, name)
     _lib = lib
@@ -739,4 +748,132 @@ def ss_tree_prune(tok: torch.Tensor, parent: torch.Tensor, prob: torch.Tensor, t
                              float(threshold), B, T, _dev(out["keep"], i32, "keep"), _dev(out["tok"], i32, "tok"),
                              _dev(out["parent"], i32, "parent"), _dev(out["old_index"], i32, "old_index"),
                              _dev(out["n_nodes"], i32, "n_nodes"), _stream()))
+    return out
+
+
+# ------------------------------------------------------------------ n5: the cache in microscaling formats
+
+def _mx_cache(k_cache, k_scale, v_cache, v_scale, block_table, B, Hkv, D):
+    """(format, num_pages, page, max_pages, pointers) of a cache of Hkv heads of D features: the format follows from the
+    bytes of a row."""
+    P, _, page, row = k_cache.shape
+    if row not in (D, D // 2):
+        raise ValueError("rows of k_cache must be D bytes (8 bits) or D/2 (4 bits)")
+    if k_cache.shape != (P, Hkv, page, row) or v_cache.shape != k_cache.shape:
+        raise ValueError("k_cache and v_cache must be [P,Hkv,page,D or D/2]")
+    if k_scale.shape != (P, Hkv, page, D // 32) or v_scale.shape != k_scale.shape:
+        raise ValueError("k_scale and v_scale must be [P,Hkv,page,D/32]")
+    if block_table.shape[0] != B:
+        raise ValueError("block_table batch size mismatch")
+    u8 = torch.uint8
+    ptrs = (_dev(k_cache, u8, "k_cache"), _dev(k_scale, u8, "k_scale"), _dev(v_cache, u8, "v_cache"), _dev(v_scale, u8, "v_scale"),
+            _dev(block_table, torch.int32, "block_table"))
+    return SS_KV_MXFP8 if row == D else SS_KV_MXFP4, P, page, block_table.shape[1], ptrs
+
+
+def ss_kv_cache_mx(num_pages: int, Hkv: int, page: int, D: int, format: int, device):
+    """An empty cache: (k_cache, k_scale, v_cache, v_scale), zeros throughout."""
+    if format not in (SS_KV_MXFP8, SS_KV_MXFP4):
+        raise ValueError("format must be SS_KV_MXFP8 or SS_KV_MXFP4")
+    row = D if format == SS_KV_MXFP8 else D // 2
+    return tuple(torch.zeros((num_pages, Hkv, page, n), dtype=torch.uint8, device=device) for n in (row, D // 32, row, D // 32))
+
+
+def _lens(t, B, name):
+    if t.shape != (B,):
+        raise ValueError("%s must be [B]" % name)
+    return _dev(t, torch.int32, name)
+
+
+def ss_kv_append_mx(k_rows, v_rows, k_cache, k_scale, v_cache, v_scale, block_table, seq_lens, n_rows,
+                    new_seq_lens: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """n5.  k_rows, v_rows [B,S,Hkv,D] (bf16 or fp32): the first n_rows[b] of sequence b are quantised to the positions from
+    seq_lens[b] on.  Returns new_seq_lens [B]."""
+    B, S, Hkv, D = k_rows.shape
+    if v_rows.shape != k_rows.shape:
+        raise ValueError("k_rows and v_rows must have one shape")
+    fmt, P, page, max_pages, ptrs = _mx_cache(k_cache, k_scale, v_cache, v_scale, block_table, B, Hkv, D)
+    if new_seq_lens is None:
+        new_seq_lens = torch.empty_like(seq_lens)
+    _check(load_library().ss_kv_append_mx(
+        _dev(k_rows, k_rows.dtype, "k_rows"), _dev(v_rows, k_rows.dtype, "v_rows"), *ptrs, max_pages, P, _lens(seq_lens, B, "seq_lens"),
+        _lens(n_rows, B, "n_rows"), B, S, Hkv, D, page, _dtype_code(k_rows), fmt, _lens(new_seq_lens, B, "new_seq_lens"), _stream()))
+    return new_seq_lens
+
+
+def ss_kv_commit_mx(k_new, v_new, k_cache, k_scale, v_cache, v_scale, block_table, seq_lens, path, n_accept, gamma: int,
+                    new_seq_lens: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """n5.  ss_kv_commit for a cache in a microscaling format.  k_new, v_new [B,R,Hkv,D] bf16 or fp32; path [B,max_depth+1] and
+    n_accept [B] as ss_tree_verify returns them.  Returns new_seq_lens [B]."""
+    B, R, Hkv, D = k_new.shape
+    T = R // (1 + gamma)
+    if R != T * (1 + gamma) or v_new.shape != k_new.shape:
+        raise ValueError("k_new / v_new must be [B,T*(1+gamma),Hkv,D]")
+    if path.dim() != 2 or path.shape[0] != B:
+        raise ValueError("path must be [B,max_depth+1]")
+    fmt, P, page, max_pages, ptrs = _mx_cache(k_cache, k_scale, v_cache, v_scale, block_table, B, Hkv, D)
+    if new_seq_lens is None:
+        new_seq_lens = torch.empty_like(seq_lens)
+    _check(load_library().ss_kv_commit_mx(
+        _dev(k_new, k_new.dtype, "k_new"), _dev(v_new, k_new.dtype, "v_new"), *ptrs, max_pages, P, _lens(seq_lens, B, "seq_lens"),
+        _dev(path, torch.int32, "path"), _lens(n_accept, B, "n_accept"), B, T, gamma, Hkv, D, page, path.shape[1] - 1,
+        _dtype_code(k_new), fmt, _lens(new_seq_lens, B, "new_seq_lens"), _stream()))
+    return new_seq_lens
+
+
+def ss_kv_read_mx(k_cache, k_scale, v_cache, v_scale, block_table, seq_lens, k_rows, v_rows, first: Optional[torch.Tensor] = None):
+    """n5.  Rows k_rows, v_rows [B,S,Hkv,D] (bf16 or fp32) get what the positions first[b].. (default 0..) below seq_lens[b]
+    hold; rows behind those are left as they are.  Returns (k_rows, v_rows)."""
+    B, S, Hkv, D = k_rows.shape
+    if v_rows.shape != k_rows.shape:
+        raise ValueError("k_rows and v_rows must have one shape")
+    fmt, P, page, max_pages, ptrs = _mx_cache(k_cache, k_scale, v_cache, v_scale, block_table, B, Hkv, D)
+    _check(load_library().ss_kv_read_mx(
+        *ptrs, max_pages, P, None if first is None else _lens(first, B, "first"), _lens(seq_lens, B, "seq_lens"), B, S, Hkv, D, page,
+        _dtype_code(k_rows), fmt, _dev(k_rows, k_rows.dtype, "k_rows"), _dev(v_rows, k_rows.dtype, "v_rows"), _stream()))
+    return k_rows, v_rows
+
+
+def ss_msa_mx_workspace_bytes(B, T, gamma, H, Hkv, D, max_seq_len) -> int:
+    return load_library().ss_msa_mx_workspace_bytes(B, T, gamma, H, Hkv, D, max_seq_len)
+
+
+def ss_msa_mx_plan(B, T, gamma, H, Hkv, D, max_seq_len):
+    """(most splits of a sequence, query rows per workgroup) of an ss_msa_attention_mx call of this shape."""
+    n, rows = ctypes.c_int(0), ctypes.c_int(0)
+    _check(load_library().ss_msa_mx_plan(B, T, gamma, H, Hkv, D, max_seq_len, ctypes.byref(n), ctypes.byref(rows)))
+    return n.value, rows.value
+
+
+def ss_msa_mx_workspace(B, T, gamma, H, Hkv, D, max_seq_len, device) -> torch.Tensor:
+    """A zero-filled workspace for ss_msa_attention_mx calls of this shape (zero before the first call, as every call leaves
+    the part that has to be)."""
+    need = ss_msa_mx_workspace_bytes(B, T, gamma, H, Hkv, D, max_seq_len)
+    return ss_msa_workspace_init(torch.empty(max(need, 1), dtype=torch.uint8, device=device))
+
+
+def ss_msa_attention_mx(q, k_new, v_new, k_cache, k_scale, v_cache, v_scale, block_table, seq_lens, parent, gamma: int, scale: float,
+                        flags: int = 0, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                        n_nodes: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """n5, a2 over a cache in a microscaling format.  q [B,R,H,D]; k_new, v_new [B,R,Hkv,D] (bf16); k_cache, v_cache
+    [P,Hkv,page,D or D/2], k_scale, v_scale [P,Hkv,page,D/32] uint8; the others as ss_msa_attention takes them, `n_nodes`
+    included.  `workspace`: a tensor from ss_msa_mx_workspace; made here if not given.  Returns out [B,R,H,D]."""
+    B, R, H, D = q.shape
+    Hkv, T = k_new.shape[2], parent.shape[1]
+    if R != T * (1 + gamma) or k_new.shape != (B, R, Hkv, D) or v_new.shape != (B, R, Hkv, D):
+        raise ValueError("q / k_new / v_new shapes do not match B,R,H,Hkv,D")
+    if parent.shape[0] != B:
+        raise ValueError("parent batch size mismatch")
+    fmt, P, page, max_pages, ptrs = _mx_cache(k_cache, k_scale, v_cache, v_scale, block_table, B, Hkv, D)
+    if out is None:
+        out = torch.empty_like(q)
+    elif out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    if workspace is None:
+        workspace = ss_msa_mx_workspace(B, T, gamma, H, Hkv, D, max_pages * page, q.device)
+    bf = torch.bfloat16
+    _check(load_library().ss_msa_attention_mx(
+        _dev(q, bf, "q"), _dev(k_new, bf, "k_new"), _dev(v_new, bf, "v_new"), *ptrs, max_pages, P, _lens(seq_lens, B, "seq_lens"),
+        _dev(parent, torch.int32, "parent"), None if n_nodes is None else _lens(n_nodes, B, "n_nodes"), B, T, gamma, H, Hkv, D, page,
+        float(scale), fmt, flags, _dev(out, bf, "out"), _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()))
     return out

@@ -1,0 +1,128 @@
+"""The calls on a cache in a microscaling format refuse what they cannot do before anything is enqueued (no GPU needed), and the
+binding refuses tensors whose shapes or types do not fit together."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2402_11131_amd import api
+
+P = ctypes.c_void_p(4096)      # never dereferenced
+ODD = ctypes.c_void_p(4096 + 2)
+INVALID, UNSUPPORTED, WORKSPACE = 1, 2, 4
+
+
+def _call(fn, order, defaults, **kw):
+    assert set(kw) <= set(order)
+    rc = getattr(api.load_library(), fn)(*[kw.get(n, defaults.get(n, P)) for n in order])
+    return rc
+
+
+def _append(**kw):
+    order = "k_rows v_rows k_cache k_scale v_cache v_scale table max_pages num_pages seq_lens n_rows B S Hkv D page dtype format new stream"
+    return _call("ss_kv_append_mx", order.split(), dict(max_pages=8, num_pages=16, B=1, S=4, Hkv=2, D=64, page=16, dtype=1, format=1,
+                                                        new=ctypes.c_void_p(8192), stream=None), **kw)
+
+
+def _commit(**kw):
+    order = ("k_new v_new k_cache k_scale v_cache v_scale table max_pages num_pages seq_lens path n_accept B T gamma Hkv D page max_depth "
+             "dtype format new stream")
+    return _call("ss_kv_commit_mx", order.split(), dict(max_pages=8, num_pages=16, B=1, T=4, gamma=2, Hkv=2, D=64, page=16, max_depth=3,
+                                                        dtype=1, format=1, new=ctypes.c_void_p(8192), stream=None), **kw)
+
+
+def _read(**kw):
+    order = "k_cache k_scale v_cache v_scale table max_pages num_pages first seq_lens B S Hkv D page dtype format k_rows v_rows stream"
+    return _call("ss_kv_read_mx", order.split(), dict(max_pages=8, num_pages=16, first=None, B=1, S=4, Hkv=2, D=64, page=16, dtype=1,
+                                                      format=1, stream=None), **kw)
+
+
+def _attend(**kw):
+    order = ("q k_new v_new k_cache k_scale v_cache v_scale table max_pages num_pages seq_lens parent n_nodes B T gamma H Hkv D page scale "
+             "format flags out workspace workspace_bytes stream")
+    kw = dict(kw)
+    if "scale" in kw:
+        kw["scale"] = ctypes.c_float(kw["scale"])
+    return _call("ss_msa_attention_mx", order.split(), dict(max_pages=256, num_pages=16, n_nodes=None, B=1, T=4, gamma=2, H=4, Hkv=2, D=64,
+                                                            page=16, scale=ctypes.c_float(0.1), format=1, flags=0, workspace_bytes=1 << 30,
+                                                            stream=None), **kw)
+
+
+@pytest.mark.parametrize("call", [_append, _commit, _read, _attend])
+def test_what_every_call_refuses(call):
+    assert call(D=96) == UNSUPPORTED and call(D=256) == UNSUPPORTED
+    assert call(page=24) == UNSUPPORTED and b"page_size" in api.load_library().ss_last_error()
+    assert call(format=2) == UNSUPPORTED and call(format=-1) == UNSUPPORTED
+    assert call(B=-1) == INVALID and call(Hkv=0) == INVALID
+    assert call(B=65536) in (INVALID, UNSUPPORTED)
+    assert call(max_pages=0) == INVALID and call(num_pages=0) == INVALID
+    assert call(max_pages=1 << 27) == UNSUPPORTED
+    for name in ("k_cache", "k_scale", "v_cache", "v_scale", "table", "seq_lens"):
+        assert call(**{name: None}) == INVALID, name
+    for name in ("k_cache", "k_scale", "v_cache", "v_scale"):
+        assert call(**{name: ODD}) == INVALID, name
+        assert b"aligned" in api.load_library().ss_last_error()
+    assert call(B=0, k_cache=None, k_scale=None, v_cache=None, v_scale=None, table=None, seq_lens=None) == 0  # an empty batch
+
+
+def test_append_commit_and_read():
+    for call, rows in ((_append, ("k_rows", "v_rows")), (_commit, ("k_new", "v_new")), (_read, ("k_rows", "v_rows"))):
+        assert call(dtype=2) == UNSUPPORTED
+        for name in rows:
+            assert call(**{name: None}) == INVALID and call(**{name: ctypes.c_void_p(4096 + 8)}) == INVALID
+    assert _append(S=-1) == INVALID and _read(S=-1) == INVALID
+    assert _read(S=0, k_rows=None, v_rows=None) == 0
+    assert _append(n_rows=None) == INVALID
+    assert _append(new=P) == INVALID and _commit(new=P) == INVALID    # seq_lens itself
+    assert _commit(path=None) == INVALID and _commit(n_accept=None) == INVALID
+    assert _commit(T=65) == UNSUPPORTED and _commit(gamma=9) == UNSUPPORTED and _commit(max_depth=64) == INVALID
+
+
+def test_attention():
+    assert _attend(T=65) == UNSUPPORTED and _attend(T=0) == UNSUPPORTED and _attend(gamma=9) == UNSUPPORTED
+    assert _attend(H=3) == INVALID
+    assert _attend(flags=2) == INVALID and _attend(flags=8) == INVALID
+    for s in (0.0, -1.0, float("inf"), float("nan")):
+        assert _attend(scale=s) == INVALID
+    for name in ("q", "k_new", "v_new", "out"):
+        assert _attend(**{name: None}) == INVALID and _attend(**{name: ctypes.c_void_p(4096 + 8)}) == INVALID
+    assert _attend(parent=None) == INVALID
+    need = api.ss_msa_mx_workspace_bytes(1, 4, 2, 4, 2, 64, 256 * 16)
+    assert api.ss_msa_mx_plan(1, 4, 2, 4, 2, 64, 256 * 16)[0] > 1
+    assert _attend(workspace=None) == WORKSPACE and _attend(workspace_bytes=need - 1) == WORKSPACE
+    assert b"workspace" in api.load_library().ss_last_error()
+    assert api.ss_msa_mx_workspace_bytes(1, 4, 2, 4, 2, 96, 4096) == 0
+    with pytest.raises(api.SSError):
+        api.ss_msa_mx_plan(1, 65, 2, 4, 2, 64, 4096)
+
+
+def test_plan_covers_every_row_and_keeps_small_problems_whole():
+    for B, T, gamma, H, Hkv, D, n in [(1, 1, 0, 1, 1, 64, 1), (4, 16, 4, 32, 32, 128, 4096), (8, 32, 4, 32, 8, 128, 32768), (64, 1, 0, 32, 4, 128, 900)]:
+        splits, rows = api.ss_msa_mx_plan(B, T, gamma, H, Hkv, D, n)
+        assert splits >= 1 and rows % 16 == 0 and rows >= min(16, T)
+        assert splits <= max(1, -(-n // 256))
+    assert api.ss_msa_mx_plan(1, 1, 0, 1, 1, 64, 0) == (1, 16)
+    assert api.ss_msa_mx_workspace_bytes(1, 1, 0, 1, 1, 64, 200) == 256
+
+
+def test_binding_checks_shapes_and_types():
+    cache = api.ss_kv_cache_mx(4, 2, 16, 64, api.SS_KV_MXFP4, "cpu")
+    assert [tuple(t.shape) for t in cache] == [(4, 2, 16, 32), (4, 2, 16, 2)] * 2
+    table, lens = torch.zeros((1, 2), dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    rows = torch.zeros((1, 3, 2, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError):   # heads of 128 do not fit rows of 32 bytes
+        api.ss_kv_append_mx(torch.zeros((1, 3, 2, 128)), torch.zeros((1, 3, 2, 128)), *cache, table, lens, lens)
+    with pytest.raises(ValueError):   # three heads
+        api.ss_kv_append_mx(torch.zeros((1, 3, 3, 64)), torch.zeros((1, 3, 3, 64)), *cache, table, lens, lens)
+    with pytest.raises(ValueError):
+        api.ss_kv_append_mx(rows, rows[:, :2], *cache, table, lens, lens)
+    with pytest.raises(ValueError):
+        api.ss_kv_commit_mx(rows, rows, *cache, table, lens, table, lens, gamma=1)
+    with pytest.raises(ValueError):
+        api.ss_kv_read_mx(*cache, torch.zeros((2, 2), dtype=torch.int32), lens, rows, rows)
+    with pytest.raises(ValueError):
+        api.ss_msa_attention_mx(rows, rows, rows, *cache, table, lens, torch.zeros((1, 2), dtype=torch.int32), 0, 0.1)
+    with pytest.raises(ValueError):
+        api.ss_kv_cache_mx(4, 2, 16, 64, 2, "cpu")
+    with pytest.raises(TypeError):    # tensors on the host
+        api.ss_kv_append_mx(rows, rows, *cache, table, lens, lens)
