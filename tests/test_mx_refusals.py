@@ -65,6 +65,12 @@ def test_what_every_call_refuses(call):
     assert call(B=0, k_cache=None, k_scale=None, v_cache=None, v_scale=None, table=None, seq_lens=None) == 0  # an empty batch
 
 
+def test_attention_refuses_a_cache_of_more_rows_than_32_bits_count():
+    assert _attend(num_pages=(1 << 27) + 1) == UNSUPPORTED       # 2 heads of 16 rows
+    assert b"rows" in api.load_library().ss_last_error()
+    assert _attend(num_pages=1 << 27, B=0) == 0
+
+
 def test_append_commit_and_read():
     for call, rows in ((_append, ("k_rows", "v_rows")), (_commit, ("k_new", "v_new")), (_read, ("k_rows", "v_rows"))):
         assert call(dtype=2) == UNSUPPORTED
