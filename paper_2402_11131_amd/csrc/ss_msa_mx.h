@@ -36,13 +36,18 @@ struct MsaMxArgs {
   uint32_t flags;
 };
 
-constexpr int kMxMinSplit = 256;  // cached tokens of the shortest split
 constexpr float kMxLazyLog2 = 16.0f;
 
-// Tokens per split of a sequence of L.
+// Tokens per split of a sequence of L in a call that was planned with up to n_splits: a share of L, but no fewer than are worth
+// it.  One row, 8 KV heads: 128 tokens of a split take 1 us, merging two splits 2 us and each further one a quarter more, so the
+// least worthwhile length grows with the root of L.  (512 tokens: unsplit 8.7 us, halves 8.9; 1024: 12.6 and, in quarters, 9.1;
+// 4096: splits of 256 / 512 / 1024 / 2048 tokens 12.5 / 12.5 / 15.7 / 23 us.)
 SS_HD int mx_split_len(int L, int n_splits) {
+  const float root = 5.f * sqrtf((float)L);
+  const int least = root < 256.f ? 256 : (int)root & ~127;
+  if (5 * (long)L < 8 * (long)least) n_splits = 1;
   const int even = (L + n_splits - 1) / n_splits, up = (even + 127) & ~127;
-  return up < kMxMinSplit ? kMxMinSplit : up;
+  return n_splits > 1 && up < least ? least : up < 128 ? 128 : up;
 }
 
 template <int D, bool FP8>
@@ -471,7 +476,7 @@ SS_DEV void mx_put_own_values(const MsaMxArgs& a, int c0, int lane, unsigned cha
 // coherently at device scope, and a wave announces itself only when its stores have completed.  l, mx: sum and maximum of the
 // lane's query row.
 template <int D, int NT, int K, class Tile, class Dt>
-SS_DEV void mx_finish(const MsaMxArgs& a, const MxItem& m, int u, int U, int n_tiles, int lane, floatx4 (&res)[NT][K], const float (&l)[NT],
+SS_DEV void mx_finish(const MsaMxArgs& a, const MxItem& m, int u, int U, int n_tiles, int lane, const floatx4 (&res)[NT][K], const float (&l)[NT],
                       const float (&mx)[NT], Tile tile, Dt dt) {
   const int lq = lane & 15, lg = lane >> 4;
   auto store = [&](int t, const floatx4 (&v)[K], float w) {
@@ -494,52 +499,50 @@ SS_DEV void mx_finish(const MsaMxArgs& a, const MxItem& m, int u, int U, int n_t
   const int stride = U * (NT * K * 256);  // floats of a split
   float* const part = a.part_o + item * a.n_splits * stride + u * (NT * K * 256);  // [split][NT][K][64][4]
   float* const plse = a.part_lse + item * a.n_splits * (n_tiles * 16);
-  float lse[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const bool has = m.f0 + 16 * tile(t) + lq < m.F;  // (nobody reads the others' results)
-    lse[t] = mx[t] * a.scale_log2 + __log2f(l[t]);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      res[t][k] *= inv[t];
-      if (has) st16_device(part + (size_t)m.s * stride + (t * K + k) * 256 + lane * 4, res[t][k]);
-    }
-    if (lg == 0 && has) st4_device(plse + m.s * (n_tiles * 16) + 16 * tile(t) + lq, lse[t]);  // (waves of one tile write the same)
+    for (int k = 0; k < K; ++k)
+      if (has) st16_device(part + (size_t)m.s * stride + (t * K + k) * 256 + lane * 4, res[t][k] * inv[t]);
+    if (lg == 0 && has) st4_device(plse + m.s * (n_tiles * 16) + 16 * tile(t) + lq, mx[t] * a.scale_log2 + __log2f(l[t]));  // (waves of one tile write the same)
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   unsigned int* const ctr = a.arrive + item * U + u;
   unsigned int seen = 0;
   if (lane == 0) seen = atomicAdd(ctr, 1u);
   if (__builtin_amdgcn_readfirstlane(seen) + 1 != (unsigned)m.n_active) return;
+  constexpr int AHEAD = K == 8 ? 2 : 4;  // splits whose results are asked for at once, its own (kept they cost too many registers) among them
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    floatx4 acc[K], o[K];
-    float M = -INFINITY, wsum = 0.f, lo = 0.f;
+    floatx4 acc[K];
+    float M = -INFINITY, wsum = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) acc[k] = floatx4{0.f, 0.f, 0.f, 0.f};
-    auto fetch = [&](int sp) {
+    for (int sp = 0; sp < m.n_active; sp += AHEAD) {
+      floatx4 o[AHEAD][K];
+      float lo[AHEAD];
 #pragma unroll
-      for (int k = 0; k < K; ++k) o[k] = ld16_device(part + (size_t)sp * stride, (uint32_t)((t * K + k) * 1024 + lane * 16));
-      lo = ld4_device(plse, (uint32_t)((sp * n_tiles + tile(t)) * 64 + lq * 4));
-    };
-    fetch(m.s == 0 ? 1 : 0);
-    for (int sp = 0; sp < m.n_active; ++sp) {
-      const bool mine = sp == m.s;
-      const float lk = mine ? lse[t] : lo;
-      const bool use = lk != -INFINITY;  // (a NaN counts)
-      const float m_new = use ? fmaxf(M, lk) : M;
-      const float keep = use ? exp2f(M - m_new) : 1.f, wt = use ? exp2f(lk - m_new) : 0.f;
+      for (int i = 0; i < AHEAD; ++i) {
+        const int from = sp + i;
+        if (from >= m.n_active) break;
+        lo[i] = ld4_device(plse, (uint32_t)((from * n_tiles + tile(t)) * 64 + lq * 4));
 #pragma unroll
-      for (int k = 0; k < K; ++k)
+        for (int k = 0; k < K; ++k) o[i][k] = ld16_device(part + (size_t)from * stride, (uint32_t)((t * K + k) * 1024 + lane * 16));
+      }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float v = mine ? res[t][k][e] : o[k][e];
-          acc[k][e] = use ? __builtin_fmaf(v, wt, acc[k][e] * keep) : acc[k][e];
-        }
-      wsum = __builtin_fmaf(wsum, keep, wt);
-      M = m_new;
-      const int next = sp + 1 == m.s ? sp + 2 : sp + 1;  // the next that is not this one's own
-      if (!mine && next < m.n_active) fetch(next);
+      for (int i = 0; i < AHEAD; ++i) {
+        if (sp + i >= m.n_active) break;
+        const bool use = lo[i] != -INFINITY;  // (a NaN counts)
+        const float m_new = use ? fmaxf(M, lo[i]) : M;
+        const float keep = use ? exp2f(M - m_new) : 1.f, wt = use ? exp2f(lo[i] - m_new) : 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[k][e] = use ? __builtin_fmaf(o[i][k][e], wt, acc[k][e] * keep) : acc[k][e];
+        wsum = __builtin_fmaf(wsum, keep, wt);
+        M = m_new;
+      }
     }
     store(t, acc, wsum > 0.f ? 1.f / wsum : 0.f);
   }

@@ -281,13 +281,13 @@ static MxPlan mx_plan(int B, int R, int H, int Hkv, int D, int max_len) {
   }
   const long items = (long)B * Hkv * p.n_qc;
   const int len = max_len < 1 ? 1 : max_len;
-  // Splits: as if all sequences were as long as they may get, rounds of the chip times what a workgroup takes: its tokens and,
-  // for what it does once, some 512 more (15 us; 128 and 2048 choose almost the same).  Four sequences of 4096 tokens and 32
+  // Splits: as if all sequences were as long as they may get, rounds of the chip times what a workgroup takes, its tokens and,
+  // for what it does once, some 512 more (128 and 2048 choose almost the same); and merging them (see mx_split_len).  Four sequences of 4096 tokens and 32
   // heads, 80 rows: 2 splits 43 us, 4 splits 61.  Eight of up to 32768 and 8 heads, 640 rows: 2 splits 931 us, 3 splits 756.
   long n = 1, best = 0;
-  const int most = items * units * (long)sizeof(unsigned int) <= (long)kArriveRegionBytes ? min(ceil_div(len, kMxMinSplit), 64) : 1;
+  const int most = items * units * (long)sizeof(unsigned int) <= (long)kArriveRegionBytes ? ceil_div(len, mx_split_len(len, len)) : 1;
   for (int i = 1; i <= most; ++i) {
-    const long cost = (items * i + resident - 1) / resident * (ceil_div(len, i) + 512);
+    const long cost = (items * i + resident - 1) / resident * (ceil_div(len, i) + 512) + (i > 1 ? 128 + 50 * i : 0);
     if (i == 1 || cost < best) {
       best = cost;
       n = i;
