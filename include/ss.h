@@ -9,10 +9,11 @@
  * of Eq. 4 / the attention-mask figure of the appendix), the LM head turns the
  * last hidden states into logits, the longest draft path the main stream agrees
  * with is accepted, and the streams of the last accepted node give the next
- * tree draft.  The calls a1..a5 below are those pieces; n1..n4 are the rows
+ * tree draft.  The calls a1..a5 below are those pieces; n1..n5 are the rows
  * around them: the dense projections of a layer, the parallel tree-pruning layer
- * (Sec. 3.2.3), the commit of the accepted path to the KV cache (Appendix A.1)
- * and the insertion of the stream rows (Eq. 3).
+ * (Sec. 3.2.3), the commit of the accepted path to the KV cache (Appendix A.1),
+ * the insertion of the stream rows (Eq. 3), and the cache in microscaling formats
+ * with the attention over it.
  *
  * Conventions (all calls)
  *  - extern "C", plain pointers and sizes.  Unless a parameter says "host",
@@ -721,7 +722,7 @@ int ss_kv_read_mx(const void* k_cache, const void* k_scale, const void* v_cache,
  * own rows k_new, v_new are attended to as they are given; q, k_new, v_new and out are
  * SS_BF16 (16-byte aligned).  Scores use the queries without further rounding but for
  * parts of a query below 2^-22 of its largest feature; sums, softmax and accumulation
- * are fp32, and the probabilities are rounded to bf16 as in a2.  One kernel.
+ * are fp32, and the probabilities are rounded to bf16 as in a2.  One kernel launch.
  * Limits: those of a2 and n5; num_pages*Hkv*page_size <= 2^32; flags:
  * SS_STREAM_EXCLUDE_SELF only.
  * A sequence is cut into splits of equal length, chosen from its own length and

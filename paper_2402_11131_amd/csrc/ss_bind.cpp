@@ -23,6 +23,7 @@ decltype(&ss_kv_read_mx) g_read;
 decltype(&ss_msa_attention_mx) g_attend;
 
 struct Raised {};  // a Python exception is set
+thread_local int g_on;  // device of the call's tensors; -1 before the first
 #define REFUSE(type, ...)           \
   do {                              \
     PyErr_Format(type, __VA_ARGS__); \
@@ -39,6 +40,9 @@ const char* name_of(at::ScalarType t) {
 void* ptr(const at::Tensor& t, at::ScalarType type, const char* name) {
   if (!(t.is_cuda() && t.is_contiguous() && t.scalar_type() == type))
     REFUSE(PyExc_TypeError, "%s must be a contiguous GPU tensor of dtype %s", name, name_of(type));
+  const int on = t.device().index();
+  if (g_on < 0) g_on = on;
+  if (on != g_on) REFUSE(PyExc_ValueError, "%s is on device %d, tensors before it on device %d", name, on, g_on);
   return t.data_ptr();
 }
 int32_t* ints(const at::Tensor& t, const char* name) { return (int32_t*)ptr(t, at::kInt, name); }
@@ -94,10 +98,17 @@ struct Cache {  // the format follows from the bytes of a row
   }
 };
 
-// Asked for once the tensors are known to be fit: without a GPU it is their refusal that a caller should see.
+// The current stream, of the device that the tensors are on.  Asked for once they are known to be fit: without a GPU it is
+// their refusal that a caller should see.
 void* stream() {
   PyObject* dev = PyObject_CallNoArgs(g_device);
   if (!dev) throw Raised();
+  const long current = PyLong_AsLong(dev);
+  if (current != g_on) {
+    Py_DECREF(dev);
+    if (!PyErr_Occurred()) PyErr_Format(PyExc_ValueError, "tensors on device %d, but the current device is %ld", g_on, current);
+    throw Raised();
+  }
   PyObject* st = PyObject_CallOneArg(g_stream, dev);
   Py_DECREF(dev);
   if (!st) throw Raised();
@@ -129,6 +140,7 @@ PyObject* guarded(Py_ssize_t n, Py_ssize_t want, F f) {
     PyErr_Format(PyExc_TypeError, "%zd arguments, %zd wanted", n, want);
     return nullptr;
   }
+  g_on = -1;
   try {
     return f();
   } catch (const Raised&) {
@@ -170,8 +182,8 @@ PyObject* commit(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor &k = tensor(a[0], "k_new"), &v = tensor(a[1], "v_new"), &path = tensor(a[8], "path");
     four(k, "k_new");
     const int gamma = number(a[10], "gamma");
-    const int64_t B = k.size(0), R = k.size(1), Hkv = k.size(2), D = k.size(3), T = gamma < 0 ? 0 : R / (1 + (int64_t)gamma);
-    if (gamma < 0 || R != T * (1 + gamma) || !v.sizes().equals(k.sizes())) REFUSE(PyExc_ValueError, "k_new / v_new must be [B,T*(1+gamma),Hkv,D]");
+    const int64_t B = k.size(0), R = k.size(1), Hkv = k.size(2), D = k.size(3), per = 1 + (int64_t)gamma, T = gamma < 0 ? 0 : R / per;
+    if (gamma < 0 || R != T * per || !v.sizes().equals(k.sizes())) REFUSE(PyExc_ValueError, "k_new / v_new must be [B,T*(1+gamma),Hkv,D]");
     if (path.dim() != 2 || path.size(0) != B) REFUSE(PyExc_ValueError, "path must be [B,max_depth+1]");
     const Cache c(a + 2, B, Hkv, D);
     const int dtype = row_type(k);
@@ -225,6 +237,7 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void *qp = ptr(q, at::kBFloat16, "q"), *kp = ptr(k, at::kBFloat16, "k_new"), *vp = ptr(v, at::kBFloat16, "v_new");
     int32_t *sl = lens(a[8], B, "seq_lens"), *pa = ints(parent, "parent"), *nn = a[15] == Py_None ? nullptr : lens(a[15], B, "n_nodes");
     void* op = ptr(o, at::kBFloat16, "out");
+    void* const st = stream();
     Owned made{nullptr};
     if (a[14] == Py_None) {
       PyObject* dev = PyObject_GetAttrString(a[0], "device");
@@ -237,7 +250,7 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* wp = ptr(ws, at::kByte, "workspace");
     checked(g_attend(qp, kp, vp, c.k, c.ks, c.v, c.vs, c.table, c.max_pages, c.num_pages, sl, pa, nn, small(B, "B"), small(T, "T"), gamma,
                      small(H, "H"), small(Hkv, "Hkv"), small(D, "D"), c.page, (float)scale, c.format, (uint32_t)flags, op, wp,
-                     (size_t)ws.numel(), stream()));
+                     (size_t)ws.numel(), st));
     return out.out();
   });
 }

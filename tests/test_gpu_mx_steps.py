@@ -226,3 +226,20 @@ def test_the_binding_refuses_on_the_device_too():
     assert torch.all(out == 3.0)
     api.ss_msa_attention_mx(*good, 1, 0.1, out=out)
     assert torch.isfinite(out).all() and not torch.any(out == 3.0)
+
+
+def test_tensors_of_another_device_than_the_current_one_are_refused(monkeypatch):
+    """With one GPU at hand the current device is what is made up."""
+    _, d = ref.problem(66, 1, 2, 1, 4, 2, 64, 16, (40,), FP8)
+    args = (d["q"], d["k_new"], d["v_new"], *d["cache"], d["table"], d["lens"], d["parent"], 1, 0.1)
+    want = api.ss_msa_attention_mx(*args)
+    monkeypatch.setattr(api, "_device", lambda: 1)
+    monkeypatch.setattr(api, "_bind", None)
+    with pytest.raises(ValueError, match="current device"):
+        api.ss_msa_attention_mx(*args)
+    rows = torch.zeros((1, 40, 2, 64), device=DEV)
+    with pytest.raises(ValueError, match="current device"):
+        api.ss_kv_read_mx(*d["cache"], d["table"], d["lens"], rows, rows.clone())
+    monkeypatch.undo()
+    api._bind = None
+    assert torch.equal(api.ss_msa_attention_mx(*args), want)
