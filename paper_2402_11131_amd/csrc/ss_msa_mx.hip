@@ -4,7 +4,10 @@
 // A workgroup of four wavefronts owns one (sequence, KV head, split of the cached tokens); the query heads of a group are folded
 // into the rows, of which there are 16 NT, NT = 1 or 2.  Every wave holds ALL rows (queries, running maximum and sum, outputs in
 // registers) and walks blocks of 32 keys of its own, so what is done once per key, above all turning values into bf16, is done
-// by one wave only, and the waves need nothing from each other until their results are merged.  Bound by the bytes of the cache.
+// by one wave only, and the waves need nothing from each other until their results are merged.  Bound by the bytes of the cache:
+// one row, 32 sequences of 16384 tokens, 8 KV heads of 128 in 4 bits (570 MB) 101 us, 5.7 TB/s; with sequences of 1001 to 8003
+// (157 MB) 36.5 us, of which 6 before the first block and 3 for merging.  One sequence of 411 tokens: 8.8 us, eight dependent
+// trips to memory.
 //
 // Memory pipeline.  Every wave has two rings of raw blocks in LDS, keys and values each with their scales.  Direct global-to-LDS
 // loads fill them; a wave waits for its own loads by count and nobody waits at a barrier.  Rows lie there as in the page, their
@@ -265,14 +268,19 @@ struct MxPlan {
 static MxPlan mx_plan(int B, int R, int H, int Hkv, int D, int max_len) {
   MxPlan p;
   const int F = (H / Hkv) * R, tiles = ceil_div(F, 16);
-  int units, resident;
+  int units, resident;  // waves of a workgroup that merge; workgroups that the chip holds
+  // One or two query tiles: keys of their own, us against keys shared by three waves: four sequences of 4096 tokens, 32 heads, 16
+  // rows 22.5 / 24.5, 32 rows 27.2 / 27.2; one of 2000, 8 heads, 11.2 / 14.1 and 14.3 / 15.4; heads of 64, 17.5 / 18.5 and 19.7 /
+  // 21.5; sixteen in 8 bits 69.4 / 66.4 and 67.7 / 70.5.
   if (tiles <= 2) {
     p.kernel = MxKernel{tiles, 1};
     p.n_qc = 1;
-    units = 4;
-    resident = tiles == 1 ? 768 : 512;  // workgroups that the chip holds
+    units = kMxWaves;
+    resident = tiles == 1 ? 768 : 512;
   } else {
-    const int per_wg = tiles <= 5 ? 5 : 8;  // query tiles, at most
+    // Up to five: a wave each, and two to four groups.  More: two per wave and as few chunks as there can be of up to eight (five
+    // tiles that way: 51 us, 41 the other; four sequences of 4096 tokens, 32 heads).
+    const int per_wg = tiles <= 5 ? 5 : 8;
     p.n_qc = ceil_div(tiles, per_wg);
     const int per = ceil_div(tiles, p.n_qc), nt = per <= 5 ? 1 : 2, nw = ceil_div(per, nt);
     p.kernel = MxKernel{nt, nw};
@@ -282,8 +290,9 @@ static MxPlan mx_plan(int B, int R, int H, int Hkv, int D, int max_len) {
   const long items = (long)B * Hkv * p.n_qc;
   const int len = max_len < 1 ? 1 : max_len;
   // Splits: as if all sequences were as long as they may get, rounds of the chip times what a workgroup takes, its tokens and,
-  // for what it does once, some 512 more (128 and 2048 choose almost the same); and merging them (see mx_split_len).  Four sequences of 4096 tokens and 32
-  // heads, 80 rows: 2 splits 43 us, 4 splits 61.  Eight of up to 32768 and 8 heads, 640 rows: 2 splits 931 us, 3 splits 756.
+  // for what it does once, some 512 more (128 and 2048 choose almost the same); and merging them (see mx_split_len).  Four
+  // sequences of 4096 tokens and 32 heads, 80 rows: 2 splits 43 us, 4 splits 61.  Eight of 32768 and 8 heads, 640 rows: 2 splits
+  // 931 us, 3 splits 756.
   long n = 1, best = 0;
   const int most = items * units * (long)sizeof(unsigned int) <= (long)kArriveRegionBytes ? ceil_div(len, mx_split_len(len, len)) : 1;
   for (int i = 1; i <= most; ++i) {

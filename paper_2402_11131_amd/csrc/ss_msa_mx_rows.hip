@@ -13,10 +13,10 @@
 // last to every barrier (NT = 2, eight of up to 32768 tokens, 640 rows: 1354 us, 1017 with quarters).  What a wave takes of a raw
 // block is read before the barrier and used behind it (939 us).
 //
-// Per 16 rows and 32 keys (D 128, 4 bits) 12 matrix instructions, 256 cycles of a SIMD, and 40 to 63 vector instructions; 10 KB
-// read from LDS (6 with NT = 2).  Counters: matrix pipe busy 25 % (NT = 1), vector instructions 34 %, LDS 31 %, half of the waves'
-// time waiting: what bounds it is the chain from barrier to barrier, 1 us, of two to three waves per SIMD that hide too little
-// of it for each other.  Four sequences of 4096 tokens, 32 heads, 80 rows: 43 us, 500 TFLOP/s; 640 rows: 756 us, 910 TFLOP/s.
+// Per 16 rows and 32 keys (D 128, 4 bits) 12 matrix instructions, 256 cycles of a SIMD, and 64 (NT = 1) or 49 (NT = 2) vector
+// instructions; 10 or 6 KB read from LDS.  NT = 2, eight sequences of 32768 tokens, 640 rows: 667 us, 1030 TFLOP/s; matrix pipe 43 %
+// and vector instructions 49 % of the cycles, which overlap little.  NT = 1, four of 4096, 32 heads, 80 rows: 41 us, 525 TFLOP/s;
+// 32 % and 44 %, 0.9 us from barrier to barrier: two to three waves per SIMD hide too little of each other's chain.
 #include "ss_msa_mx.h"
 
 #include <mutex>
