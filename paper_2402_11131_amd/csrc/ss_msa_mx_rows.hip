@@ -215,15 +215,19 @@ __global__ __launch_bounds__(64 * NW * G, (MxRowsShape<D, FP8, NW, NT, G>::PER_S
       __syncthreads();
       if (loader && DEPTH < n_mine) issue(DEPTH, 0);
       int slot = 1;  // of block it + 1
-      for (int it = 0; it < n_mine; ++it) {
+      // STEADY: more than DEPTH blocks follow, so nothing has to be asked.  A loop of its own (us without and with it: 640 rows,
+      // eight sequences of 32768 tokens, 667 and 647; 80 rows, four of 4096, 41.0 and 40.2) where registers allow two.
+      constexpr bool TWO_LOOPS = NT == 2 || D == 64 || !FP8;
+      auto pass = [&](int it, auto steady) {
+        constexpr bool STEADY = decltype(steady)::value;
         const int next = slot + 1 == DEPTH ? 0 : slot + 1, more = n_mine - 1 - it;  // blocks of the group after this one
-        if (loader && more > DEPTH) {  // block it + 1 has been read before the barrier
+        if (loader && (STEADY || more > DEPTH)) {  // block it + 1 has been read before the barrier
           if (((it + 1 + DEPTH) & 63) == 0) load_rows(it + 1 + DEPTH);
           issue(it + 1 + DEPTH, slot);
         }
         unsigned char* const set = tiles + (it & 1) * (NB * 2048);
         unsigned char* const set_next = tiles + ((it & 1) ^ 1) * (NB * 2048);
-        const int seen = more == 0 ? 0 : ragged && more == 1 ? tail : 32;  // of the next block's keys
+        const int seen = STEADY ? 32 : more == 0 ? 0 : ragged && more == 1 ? tail : 32;  // of the next block's keys
         if constexpr (decltype(with_rows)::value) {
           // Values are asked for LEAD feature tiles ahead, the first before all else: read where they are used, every matrix
           // instruction waits for LDS, and the compiler would put them there (NT = 2, 640 rows: 757 us, 667 with two tiles ahead, 700
@@ -259,7 +263,7 @@ __global__ __launch_bounds__(64 * NW * G, (MxRowsShape<D, FP8, NW, NT, G>::PER_S
             if (dt + LEAD < DT) V[dt % LEAD] = value(dt + LEAD);
             __builtin_amdgcn_sched_barrier(0);
           }
-          if (seen < 32) {
+          if (!STEADY && seen < 32) {
             if constexpr (decltype(with_share)::value)
               if (more == 1) put_tail(set_next, seen);
             mx_mask_tail<NT>(S, lg, seen);
@@ -271,14 +275,18 @@ __global__ __launch_bounds__(64 * NW * G, (MxRowsShape<D, FP8, NW, NT, G>::PER_S
           take(ring + next * UNIT, with_rows, with_share);
         }
         if (loader) {  // block it + 3 has landed; those after it, up to it + 1 + DEPTH, may still be under way
-          if (more > DEPTH) wait_vmcnt<(DEPTH - 2) * LPW>();
+          if (STEADY || more > DEPTH) wait_vmcnt<(DEPTH - 2) * LPW>();
           else if (DEPTH > 4 && more == 5) wait_vmcnt<2 * LPW>();
           else if (DEPTH > 3 && more == 4) wait_vmcnt<LPW>();
           else wait_vmcnt<0>();
         }
         __syncthreads();
         slot = next;
-      }
+      };
+      int it = 0;
+      if constexpr (TWO_LOOPS)
+        for (; it + DEPTH + 1 < n_mine; ++it) pass(it, std::true_type{});
+      for (; it < n_mine; ++it) pass(it, std::false_type{});
     };
     if (live) {
       if (NW <= NB || wt < NB) walk(std::true_type{}, std::true_type{});
