@@ -14,8 +14,8 @@
 // block is read before the barrier and used behind it (939 us).
 //
 // Per 16 rows and 32 keys (D 128, 4 bits) 12 matrix instructions, 256 cycles of a SIMD, and 64 (NT = 1) or 49 (NT = 2) vector
-// instructions; 10 or 6 KB read from LDS.  NT = 2, eight sequences of 32768 tokens, 640 rows: 667 us, 1030 TFLOP/s; matrix pipe 43 %
-// and vector instructions 49 % of the cycles, which overlap little.  NT = 1, four of 4096, 32 heads, 80 rows: 41 us, 525 TFLOP/s;
+// instructions; 10 or 6 KB read from LDS.  NT = 2, eight sequences of 32768 tokens, 640 rows: 646 us, 1060 TFLOP/s; matrix pipe 43 %
+// and vector instructions 49 % of the cycles, which overlap little.  NT = 1, four of 4096, 32 heads, 80 rows: 40 us, 535 TFLOP/s;
 // 32 % and 44 %, 0.9 us from barrier to barrier: two to three waves per SIMD hide too little of each other's chain.
 #include "ss_msa_mx.h"
 
