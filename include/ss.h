@@ -718,11 +718,13 @@ int ss_kv_read_mx(const void* k_cache, const void* k_scale, const void* v_cache,
 
 /*
  * n5, a2 over that cache: ss_msa_attention (n_nodes NULL) or ss_msa_attention_pruned
- * (n_nodes [B]) with the cached keys and values in a microscaling format.  The step's
- * own rows k_new, v_new are attended to as they are given; q, k_new, v_new and out are
- * SS_BF16 (16-byte aligned).  Scores use the queries without further rounding but for
- * parts of a query below 2^-22 of its largest feature; sums, softmax and accumulation
- * are fp32, and the probabilities are rounded to bf16 as in a2.  One kernel launch.
+ * (n_nodes [B]) with the cached keys and values in a microscaling format.  Rows of
+ * pruned nodes are neither computed nor written, and q, k_new and v_new may hold
+ * anything there.  The step's own rows k_new, v_new are attended to as they are given;
+ * q, k_new, v_new and out are SS_BF16 (16-byte aligned).  Scores use the queries without
+ * further rounding but for parts of a query below 2^-22 of its largest feature; sums,
+ * softmax and accumulation are fp32, and the probabilities are rounded to bf16 as in
+ * a2.  One kernel launch.
  * Limits: those of a2 and n5; num_pages*Hkv*page_size <= 2^32; flags:
  * SS_STREAM_EXCLUDE_SELF only.
  * A sequence is cut into splits of equal length, chosen from its own length and

@@ -461,11 +461,14 @@ SS_DEV void mx_load_own_values(const MsaMxArgs& a, const MxItem& m, int c0, int 
 #pragma unroll
   for (int i = 0; i < 2; ++i) vf[i] = ld16(vn + min(c0 + 16 * i + (lane >> 2), a.R - 1) * ((size_t)a.c.Hkv * D));
 }
-SS_DEV void mx_put_own_values(const MsaMxArgs& a, int c0, int lane, unsigned char* tile, const uintx4 (&vf)[2]) {
+// Rows past the last and those of pruned nodes, which nobody has filled, become zeros: a NaN there would not be hidden by
+// probabilities of zero.
+SS_DEV void mx_put_own_values(const MsaMxArgs& a, const MxItem& m, int c0, int lane, unsigned char* tile, const uintx4 (&vf)[2]) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int row = 16 * i + (lane >> 2);
-    *reinterpret_cast<uintx4*>(tile + row * 64 + (((lane & 3) ^ tile_swz(row)) * 16)) = c0 + row < a.R ? vf[i] : uintx4{0u, 0u, 0u, 0u};
+    const int row = 16 * i + (lane >> 2), r = c0 + row;
+    const bool kept = (r < m.n_kept) | ((r >= a.T) & (r < a.T + m.n_kept * a.gamma));
+    *reinterpret_cast<uintx4*>(tile + row * 64 + (((lane & 3) ^ tile_swz(row)) * 16)) = kept ? vf[i] : uintx4{0u, 0u, 0u, 0u};
   }
 }
 

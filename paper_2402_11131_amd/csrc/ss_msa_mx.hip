@@ -116,7 +116,7 @@ __global__ __launch_bounds__(64 * kMxWaves, (MxShape<D, FP8, NT>::WGS)) void msa
 #pragma unroll
       for (int np = 0; np < NB; ++np) {
         in_order();
-        mx_put_own_values(a, c0, lane, tiles + (np % TL) * 2048, vf[np]);
+        mx_put_own_values(a, m, c0, lane, tiles + (np % TL) * 2048, vf[np]);
         in_order();
         add_values(np, P);
       }
@@ -294,7 +294,7 @@ static MxPlan mx_plan(int B, int R, int H, int Hkv, int D, int max_len) {
   // sequences of 4096 tokens and 32 heads, 80 rows: 2 splits 43 us, 4 splits 61.  Eight of 32768 and 8 heads, 640 rows: 2 splits
   // 931 us, 3 splits 756.
   long n = 1, best = 0;
-  const int most = items * units * (long)sizeof(unsigned int) <= (long)kArriveRegionBytes ? ceil_div(len, mx_split_len(len, len)) : 1;
+  const int most = items * units * (long)sizeof(unsigned int) <= (long)kArriveRegionBytes ? min(ceil_div(len, mx_split_len(len, len)), 256) : 1;
   for (int i = 1; i <= most; ++i) {
     const long cost = (items * i + resident - 1) / resident * (ceil_div(len, i) + 512) + (i > 1 ? 128 + 50 * i : 0);
     if (i == 1 || cost < best) {

@@ -134,7 +134,7 @@ __global__ __launch_bounds__(64 * NW * G, (MxRowsShape<D, FP8, NW, NT, G>::PER_S
       if (mine) {
 #pragma unroll
         for (int i = 0; i < (NB + NW - 1) / NW; ++i)
-          if (wt + i * NW < NB) mx_put_own_values(a, c0, lane, tiles + (wt + i * NW) * 2048, vf[i]);
+          if (wt + i * NW < NB) mx_put_own_values(a, m, c0, lane, tiles + (wt + i * NW) * 2048, vf[i]);
       }
       __syncthreads();
       if (mine && live) {

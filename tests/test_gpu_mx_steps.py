@@ -167,6 +167,26 @@ def test_a_captured_step():
         assert mine[3][1].tolist() == [min(a + b, 320) + min(max(c + 1, 0), 320 - min(a + b, 320)) for a, b, c in zip(lens, n, acc)]
 
 
+@pytest.mark.parametrize("T,gamma,D", [(20, 3, 128), (24, 4, 64), (6, 1, 128)])
+def test_rows_of_pruned_nodes_may_hold_anything(T, gamma, D):
+    """What the projections leave untouched for pruned nodes: NaN in their queries, keys and values changes no kept row's bits."""
+    B, kept = 3, [T, 3, 1]
+    _, d = ref.problem(67, B, T, gamma, 8, 4, D, 16, (300, 40, 0), FP8)
+    for b in range(B):
+        d["parent"][b, kept[b]:] = 0
+        d["parent"][b, 0] = -1
+    n = _gpu(np.array(kept, np.int32))
+    args = lambda d: (d["q"], d["k_new"], d["v_new"], *d["cache"], d["table"], d["lens"], d["parent"], gamma, 0.1)  # noqa: E731
+    want = api.ss_msa_attention_mx(*args(d), out=torch.full_like(d["q"], 2.0), n_nodes=n)
+    bad = {name: d[name].clone() for name in ("q", "k_new", "v_new")}
+    for x in bad.values():
+        for b in range(B):
+            x[b, kept[b]:T] = float("nan")
+            x[b, T + kept[b] * gamma:] = float("nan")
+    got = api.ss_msa_attention_mx(*args(dict(d, **bad)), out=torch.full_like(d["q"], 2.0), n_nodes=n)
+    assert torch.isfinite(want).all() and torch.equal(got, want)
+
+
 def test_two_streams_at_once():
     """Two calls that may run at the same time, each with its workspace and output: the bits of one after the other."""
     calls = []
