@@ -265,14 +265,15 @@ struct MxQuarter {
   }
   // Iteration `it`'s to the block at LDS address `to`.
   SS_DEV void issue(int it, uint32_t to, int lane) const {
-    const size_t row = __builtin_amdgcn_readlane(tab, it & 63);
+    const uint32_t row = __builtin_amdgcn_readlane(tab, it & 63);
+    const uint8_t* const from = rows + mx_row_at(row, Bk::ROWB);
     if constexpr (Bk::HL > 0) {
 #pragma unroll
-      for (int i = 0; i < Bk::HL; ++i) dma16<STREAM>(rows + row * Bk::ROWB, i ? voff1 : voff, to + at + i * 1024);
+      for (int i = 0; i < Bk::HL; ++i) dma16<STREAM>(from, i ? voff1 : voff, to + at + i * 1024);
     } else {
-      if (lane < 32) dma16<STREAM>(rows + row * Bk::ROWB, voff, to + at);
+      if (lane < 32) dma16<STREAM>(from, voff, to + at);
     }
-    if (lane < 4 * Bk::NB) dma4(scales + row * Bk::NB, (uint32_t)(4 * lane), to + sc_at);
+    if (lane < 4 * Bk::NB) dma4(scales + mx_row_at(row, Bk::NB), (uint32_t)(4 * lane), to + sc_at);
   }
 };
 

@@ -25,6 +25,9 @@ struct MxCache {
 SS_DEV int mx_page(const MxCache& c, int b, int pos) {
   return min(max(c.block_table[(size_t)b * c.max_pages + (pos >> c.page_shift)], 0), c.num_pages - 1);
 }
+// Where row `row` of a cache lies, `bytes` each.  Row indices take all 32 bits: as an int, which is what a lane's register is read
+// as, one from 2^31 on would be widened to an address far in front of the cache.
+SS_HD constexpr size_t mx_row_at(uint32_t row, int bytes) { return (size_t)row * (uint32_t)bytes; }
 // Row of a position inside the cache, in tokens of one head.
 SS_DEV size_t mx_row(const MxCache& c, int page, int h, int pos) {
   return ((size_t)page * c.Hkv + h) * c.page + (pos & (c.page - 1));
