@@ -691,10 +691,11 @@ int ss_kv_alloc_pages(int32_t* block_table, int max_pages_per_seq, const int32_t
  *  SS_BF16, 16-byte aligned) is quantised to position seq_lens[b] + j: a prompt, or
  *  the next chunk of one.  n_rows [B] is clamped to [0,S]; rows at and past it are
  *  not read.  new_seq_lens [B] out, or NULL: seq_lens[b] + number of rows written.
- *  Must not be the seq_lens array itself.
+ *  Must not share memory with seq_lens, n_rows or block_table (refused).
  *
  * ss_kv_commit_mx: ss_kv_commit for this cache; the rows of the accepted path are
- *  quantised as they are written.
+ *  quantised as they are written.  new_seq_lens must not share memory with seq_lens,
+ *  path, n_accept or block_table (refused).
  *
  * ss_kv_read_mx: row j of k_rows, v_rows [B,S,Hkv,D] (dtype as above) gets the
  *  values that position first[b] + j holds, for positions below seq_lens[b]; rows

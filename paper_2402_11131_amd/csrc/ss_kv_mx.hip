@@ -259,6 +259,10 @@ static int check_rows(const char* fn, int B, int dtype, const void* k_rows, cons
   SS_REQUIRE((((uintptr_t)k_rows | (uintptr_t)v_rows) & 15) == 0, SS_ERR_INVALID_ARG, "%s: rows not aligned to 16 bytes", fn);
   return SS_OK;
 }
+// New lengths are written while other workgroups still read what the call was given.
+static bool shares(const int32_t* out, long n_out, const int32_t* in, long n_in) {
+  return out != nullptr && (uintptr_t)out < (uintptr_t)(in + n_in) && (uintptr_t)in < (uintptr_t)(out + n_out);
+}
 
 }  // namespace ss
 
@@ -279,7 +283,9 @@ int ss_kv_append_mx(const void* k_rows, const void* v_rows, void* k_cache, void*
     if (int rc = check_rows(fn, B, dtype, k_rows, v_rows)) return rc;
   SS_REQUIRE(B <= 65535, SS_ERR_UNSUPPORTED, "%s: B=%d", fn, B);
   SS_REQUIRE(seq_lens && n_rows, SS_ERR_INVALID_ARG, "%s: NULL seq_lens or n_rows", fn);
-  SS_REQUIRE(new_seq_lens == nullptr || new_seq_lens != seq_lens, SS_ERR_INVALID_ARG, "%s: new_seq_lens must not be the seq_lens array", fn);
+  SS_REQUIRE(!shares(new_seq_lens, B, seq_lens, B) && !shares(new_seq_lens, B, n_rows, B) &&
+                 !shares(new_seq_lens, B, block_table, (long)B * max_pages_per_seq),
+             SS_ERR_INVALID_ARG, "%s: new_seq_lens shares memory with seq_lens, n_rows or block_table", fn);
   MxWriteArgs a;
   a.c = mx_cache(k_cache, k_scale, v_cache, v_scale, block_table, max_pages_per_seq, num_pages, Hkv, D, page_size);
   a.k_rows = k_rows; a.v_rows = v_rows; a.seq_lens = seq_lens; a.path = nullptr; a.count = n_rows; a.new_seq_lens = new_seq_lens;
@@ -303,7 +309,9 @@ int ss_kv_commit_mx(const void* k_new, const void* v_new, void* k_cache, void* k
   if (B == 0) return SS_OK;
   if (int rc = check_rows(fn, B, dtype, k_new, v_new)) return rc;
   SS_REQUIRE(seq_lens && path && n_accept, SS_ERR_INVALID_ARG, "%s: NULL tensor argument", fn);
-  SS_REQUIRE(new_seq_lens == nullptr || new_seq_lens != seq_lens, SS_ERR_INVALID_ARG, "%s: new_seq_lens must not be the seq_lens array", fn);
+  SS_REQUIRE(!shares(new_seq_lens, B, seq_lens, B) && !shares(new_seq_lens, B, n_accept, B) &&
+                 !shares(new_seq_lens, B, path, (long)B * (max_depth + 1)) && !shares(new_seq_lens, B, block_table, (long)B * max_pages_per_seq),
+             SS_ERR_INVALID_ARG, "%s: new_seq_lens shares memory with seq_lens, path, n_accept or block_table", fn);
   MxWriteArgs a;
   a.c = mx_cache(k_cache, k_scale, v_cache, v_scale, block_table, max_pages_per_seq, num_pages, Hkv, D, page_size);
   a.k_rows = k_new; a.v_rows = v_new; a.seq_lens = seq_lens; a.path = path; a.count = n_accept; a.new_seq_lens = new_seq_lens;
