@@ -683,7 +683,8 @@ int ss_kv_alloc_pages(int32_t* block_table, int max_pages_per_seq, const int32_t
  * rounded to nearest, ties to the even code, and keep the sign of a zero.  A value
  * is then off by at most half an element's step.  A block that holds a NaN or an
  * infinity gets s = 255 and zeros as elements, and reads as NaN.
- * Limits (all calls): D in {64,128}, page_size in {16,32,64}, B <= 65535.
+ * Limits (all calls): D in {64,128}, page_size in {16,32,64}, B <= 65535,
+ * max_pages_per_seq*page_size <= 2^30.
  * Page ids are clamped and positions at or past max_pages_per_seq*page_size
  * dropped as in ss_kv_commit.  Pages that are written must not be shared.
  *
@@ -736,7 +737,8 @@ int ss_kv_read_mx(const void* k_cache, const void* k_scale, const void* v_cache,
  * (ss_msa_workspace_init), zeros after every call, not shared by calls that may run at
  * the same time.  One workspace can serve this call and a2 in turn.
  * ss_msa_mx_plan: most splits a sequence has in a call of this shape and query rows per
- * workgroup; either pointer may be NULL.  Host-only.
+ * workgroup; either pointer may be NULL.  Host-only.  A max_seq_len above 2^30, the most
+ * that a block table may hold, counts as 2^30.
  */
 size_t ss_msa_mx_workspace_bytes(int B, int T, int gamma, int H, int Hkv, int D, int max_seq_len);
 int ss_msa_mx_plan(int B, int T, int gamma, int H, int Hkv, int D, int max_seq_len, int* n_splits,

@@ -17,7 +17,7 @@ int mx_check(const char* fn, int Hkv, int D, int page_size, int max_pages_per_se
              page_size);
   SS_REQUIRE(max_pages_per_seq >= 1 && num_pages >= 1, SS_ERR_INVALID_ARG, "%s: max_pages_per_seq=%d num_pages=%d", fn,
              max_pages_per_seq, num_pages);
-  SS_REQUIRE((long)max_pages_per_seq * page_size <= (1L << 30), SS_ERR_UNSUPPORTED, "%s: sequence capacity too large", fn);
+  SS_REQUIRE((long)max_pages_per_seq * page_size <= kMxMaxLen, SS_ERR_UNSUPPORTED, "%s: sequence capacity too large", fn);
   if (!tensors) return SS_OK;
   SS_REQUIRE(k_cache && k_scale && v_cache && v_scale && block_table, SS_ERR_INVALID_ARG, "%s: NULL tensor argument", fn);
   SS_REQUIRE((((uintptr_t)k_cache | (uintptr_t)v_cache) & 15) == 0 && (((uintptr_t)k_scale | (uintptr_t)v_scale) & 3) == 0,

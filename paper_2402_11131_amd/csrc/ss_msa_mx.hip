@@ -288,7 +288,7 @@ static MxPlan mx_plan(int B, int R, int H, int Hkv, int D, int max_len) {
     resident = nt == 1 ? 256 : 512;
   }
   const long items = (long)B * Hkv * p.n_qc;
-  const int len = max_len < 1 ? 1 : max_len;
+  const int len = min(max(max_len, 1), kMxMaxLen);
   // Splits: as if all sequences were as long as they may get, rounds of the chip times what a workgroup takes, its tokens and,
   // for what it does once, some 512 more (128 and 2048 choose almost the same); and merging them (see mx_split_len).  Four
   // sequences of 4096 tokens and 32 heads, 80 rows: 2 splits 43 us, 4 splits 61.  Eight of 32768 and 8 heads, 640 rows: 2 splits
