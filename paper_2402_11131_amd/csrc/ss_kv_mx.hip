@@ -153,7 +153,7 @@ __global__ __launch_bounds__(kMxThreads) void kv_write_mx_kernel(MxWriteArgs a) 
 
 static int launch_write(const char* fn, const MxWriteArgs& a, int B, int rows, int dtype, int format, hipStream_t st) {
   const int per_wg = kMxThreads / (a.c.D >> 3) * kMxRows;
-  SS_REQUIRE((long)ceil_div(rows, per_wg) * a.c.Hkv <= 0x7fffffffL, SS_ERR_UNSUPPORTED, "%s: grid too large", fn);
+  SS_REQUIRE((long)ceil_div(rows, per_wg) * a.c.Hkv <= kMxMaxThreads / kMxThreads, SS_ERR_UNSUPPORTED, "%s: grid too large", fn);
   const dim3 grid((unsigned)(ceil_div(rows, per_wg) * a.c.Hkv), 1, (unsigned)B);
   auto kern = dtype == SS_F32 ? (format == SS_KV_MXFP8 ? kv_write_mx_kernel<float, true> : kv_write_mx_kernel<float, false>)
                               : (format == SS_KV_MXFP8 ? kv_write_mx_kernel<uint16_t, true> : kv_write_mx_kernel<uint16_t, false>);
@@ -336,7 +336,7 @@ int ss_kv_read_mx(const void* k_cache, const void* k_scale, const void* v_cache,
   a.c = mx_cache((void*)k_cache, (void*)k_scale, (void*)v_cache, (void*)v_scale, block_table, max_pages_per_seq, num_pages, Hkv, D, page_size);
   a.first = first; a.seq_lens = seq_lens; a.k_rows = k_rows; a.v_rows = v_rows; a.S = S;
   const int per_wg = kMxThreads / (D >> 3) * kMxRows;
-  SS_REQUIRE((long)ceil_div(S, per_wg) * Hkv <= 0x7fffffffL, SS_ERR_UNSUPPORTED, "%s: grid too large", fn);
+  SS_REQUIRE((long)ceil_div(S, per_wg) * Hkv <= kMxMaxThreads / kMxThreads, SS_ERR_UNSUPPORTED, "%s: grid too large", fn);
   const dim3 grid((unsigned)(ceil_div(S, per_wg) * Hkv), 1, (unsigned)B);
   const bool stream_out = 2 * (size_t)B * S * Hkv * D * (dtype == SS_F32 ? 4 : 2) > kMxStreamBytes;
   auto kern = dtype == SS_F32 ? read_kernel<float>(format, stream_out) : read_kernel<uint16_t>(format, stream_out);

@@ -249,6 +249,7 @@ __global__ __launch_bounds__(64 * kMxWaves, (MxShape<D, FP8, NT>::WGS)) void msa
 
 template <int D, bool FP8>
 static int launch_mx(const MsaMxArgs& a, int nt, long wgs, hipStream_t st) {
+  SS_REQUIRE(wgs <= kMxMaxThreads / (64 * kMxWaves), SS_ERR_UNSUPPORTED, "ss_msa_attention_mx: grid too large");
   auto kern = nt == 1 ? msa_mx_kernel<D, FP8, 1> : msa_mx_kernel<D, FP8, 2>;
   hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(64 * kMxWaves), 0, st, a);
   return check_launch("ss_msa_attention_mx");
@@ -365,7 +366,6 @@ int ss_msa_attention_mx(const void* q, const void* k_new, const void* v_new, con
   SS_REQUIRE(plan.n_splits == 1 || (workspace != nullptr && workspace_bytes >= plan.total_bytes), SS_ERR_WORKSPACE,
              "%s: workspace of %zu bytes needed, %zu given", fn, plan.total_bytes, workspace_bytes);
   const long wgs = ((long)B * Hkv * plan.n_splits + 7) / 8 * 8 * plan.n_qc;
-  SS_REQUIRE(wgs <= 0x7fffffffL && (long)B * Hkv * plan.n_qc <= 0x7fffffffL, SS_ERR_UNSUPPORTED, "%s: grid too large", fn);
   MsaMxArgs a;
   a.q = (const uint16_t*)q; a.k_new = (const uint16_t*)k_new; a.v_new = (const uint16_t*)v_new; a.out = (uint16_t*)out;
   a.c.k = (uint8_t*)k_cache; a.c.ks = (uint8_t*)k_scale; a.c.v = (uint8_t*)v_cache; a.c.vs = (uint8_t*)v_scale;

@@ -346,6 +346,7 @@ __global__ __launch_bounds__(64 * NW * G, (MxRowsShape<D, FP8, NW, NT, G>::PER_S
 template <int D, bool FP8, int NW, int NT, int G>
 static int launch_rows(const MsaMxArgs& a, long wgs, hipStream_t st) {
   using Sh = MxRowsShape<D, FP8, NW, NT, G>;
+  SS_REQUIRE(wgs <= kMxMaxThreads / (64 * NW * G), SS_ERR_UNSUPPORTED, "ss_msa_attention_mx: grid too large");
   auto kern = msa_mx_rows_kernel<D, FP8, NW, NT, G>;
   static std::once_flag attr_once;
   static hipError_t attr_err = hipSuccess;

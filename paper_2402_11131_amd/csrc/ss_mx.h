@@ -14,6 +14,7 @@ typedef __attribute__((__vector_size__(2 * sizeof(float)))) float floatx2;
 typedef __attribute__((__vector_size__(8 * sizeof(int)))) int intx8;
 
 constexpr int kMxBlock = 32;
+constexpr long kMxMaxThreads = 0xffffffffL;  // of a launch, as the runtime counts them
 constexpr int kMxMaxLen = 1 << 30;  // tokens that a row of a block table may hold
 SS_HD int mx_row_bytes(int D, bool fp8) { return fp8 ? D : D / 2; }
 
