@@ -726,9 +726,10 @@ int ss_kv_read_mx(const void* k_cache, const void* k_scale, const void* v_cache,
  * q, k_new, v_new and out are SS_BF16 (16-byte aligned).  Scores use the queries without
  * further rounding but for parts of a query below 2^-22 of its largest feature; sums,
  * softmax and accumulation are fp32, and the probabilities are rounded to bf16 as in
- * a2.  One kernel launch.
- * Limits: those of a2 and n5; num_pages*Hkv*page_size <= 2^32; flags:
- * SS_STREAM_EXCLUDE_SELF only.
+ * a2.  The products of scale and scores are fp32 too: from about 2^24 in size on their
+ * rounding decides, and from 2^31 on results may be NaN.  One kernel launch.
+ * Limits: those of a2 and n5; num_pages*Hkv*page_size <= 2^32; scale and its product
+ * with log2(e) positive and finite; flags: SS_STREAM_EXCLUDE_SELF only.
  * A sequence is cut into splits of equal length, chosen from its own length and
  * ss_msa_mx_plan's number of splits; no other sequence changes its result.
  * workspace: at least ss_msa_mx_workspace_bytes(...) bytes with max_seq_len =

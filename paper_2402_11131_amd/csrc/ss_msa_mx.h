@@ -37,6 +37,9 @@ struct MsaMxArgs {
 };
 
 constexpr float kMxLazyLog2 = 16.0f;
+// Running maximum before the first score: below every score whose product with c = scale * log2(e) an fp32 number holds, and its
+// own product with c is one too (rows that see nothing of a block keep it, and -inf * c - (-inf) would be NaN).
+SS_DEV float mx_no_maximum(float c) { return -3e38f / fmaxf(c, 1.f); }
 
 // Tokens per split of a sequence of L in a call that was planned with up to n_splits: a share of L, but no fewer than are worth
 // it.  One row, 8 KV heads: 128 tokens of a split take 1 us, merging two splits 2 us and each further one a quarter more, so the

@@ -79,16 +79,16 @@ __global__ __launch_bounds__(64 * kMxWaves, (MxShape<D, FP8, NT>::WGS)) void msa
     }
   }
 
+  const float c = a.scale_log2, lazy_thr = kMxLazyLog2 / c, m_none = mx_no_maximum(c);
   floatx4 O[NT][DT], S[NT][2];
   float m_run[NT], l_run[NT];  // maximum of the query row, sum of this lane's probabilities
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    m_run[t] = -1e30f;
+    m_run[t] = m_none;
     l_run[t] = 0.f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) O[t][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
-  const float c = a.scale_log2, lazy_thr = kMxLazyLog2 / c;
   float pinf = INFINITY;  // see vmax2
   asm volatile("" : "+s"(pinf));
   const MxReader<D, FP8> rd(lane);
@@ -354,7 +354,7 @@ int ss_msa_attention_mx(const void* q, const void* k_new, const void* v_new, con
   const char* fn = "ss_msa_attention_mx";
   if (int rc = mx_check_shape(fn, B, T, gamma, H, Hkv, D)) return rc;
   if (int rc = mx_check(fn, Hkv, D, page_size, max_pages_per_seq, num_pages, format, k_cache, k_scale, v_cache, v_scale, block_table, B > 0)) return rc;
-  SS_REQUIRE(scale > 0.f && isfinite(scale), SS_ERR_INVALID_ARG, "%s: scale must be positive and finite", fn);
+  SS_REQUIRE(scale > 0.f && isfinite(scale * 1.4426950408889634f), SS_ERR_INVALID_ARG, "%s: scale must be positive and finite, and so its product with log2(e)", fn);
   SS_REQUIRE((flags & ~SS_STREAM_EXCLUDE_SELF) == 0, SS_ERR_INVALID_ARG, "%s: unknown flags 0x%x", fn, flags);
   SS_REQUIRE((long)num_pages * Hkv <= (1L << 32) / page_size, SS_ERR_UNSUPPORTED, "%s: a cache of more than 2^32 rows", fn);
   if (B == 0) return SS_OK;
