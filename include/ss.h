@@ -682,7 +682,9 @@ int ss_kv_alloc_pages(int32_t* block_table, int max_pages_per_seq, const int32_t
  * element lies beyond the format's largest, so none is clamped; elements are
  * rounded to nearest, ties to the even code, and keep the sign of a zero.  A value
  * is then off by at most half an element's step.  A block that holds a NaN or an
- * infinity gets s = 255 and zeros as elements, and reads as NaN.
+ * infinity gets s = 255 and zeros as elements, and reads as NaN.  Magnitudes that are
+ * rounded up to 2^128 (from 1.9375 * 2^127 on in 8 bits, from 1.75 * 2^127 on in 4) read
+ * as infinity.
  * Limits (all calls): D in {64,128}, page_size in {16,32,64}, B <= 65535,
  * max_pages_per_seq*page_size <= 2^30.
  * Page ids are clamped and positions at or past max_pages_per_seq*page_size
@@ -701,8 +703,8 @@ int ss_kv_alloc_pages(int32_t* block_table, int max_pages_per_seq, const int32_t
  * ss_kv_read_mx: row j of k_rows, v_rows [B,S,Hkv,D] (dtype as above) gets the
  *  values that position first[b] + j holds, for positions below seq_lens[b]; rows
  *  behind those are left as they are.  first [B] or NULL (0 for all); negative
- *  entries count as 0.  Values are exact in fp32, and in bf16 but for parts of an
- *  e4m3 value below 2^-133 (rounded to nearest even).
+ *  entries count as 0.  Values below 2^128 are exact in fp32, and in bf16 but for parts
+ *  of an e4m3 value below 2^-133 (rounded to nearest even).
  */
 int ss_kv_append_mx(const void* k_rows, const void* v_rows, void* k_cache, void* k_scale, void* v_cache,
                     void* v_scale, const int32_t* block_table, int max_pages_per_seq, int num_pages,
@@ -722,7 +724,9 @@ int ss_kv_read_mx(const void* k_cache, const void* k_scale, const void* v_cache,
  * n5, a2 over that cache: ss_msa_attention (n_nodes NULL) or ss_msa_attention_pruned
  * (n_nodes [B]) with the cached keys and values in a microscaling format.  Rows of
  * pruned nodes are neither computed nor written, and q, k_new and v_new may hold
- * anything there.  The step's own rows k_new, v_new are attended to as they are given;
+ * anything there.  The step's own rows k_new, v_new are attended to as they are given,
+ * and as in a2 a NaN or an infinity in a value reaches every row of its sequence and
+ * head, also those that do not see it (a NaN in a key only those that do);
  * q, k_new, v_new and out are SS_BF16 (16-byte aligned).  Scores use the queries without
  * further rounding but for parts of a query below 2^-22 of its largest feature; sums,
  * softmax and accumulation are fp32, and the probabilities are rounded to bf16 as in
