@@ -734,8 +734,9 @@ int ss_kv_read_mx(const void* k_cache, const void* k_scale, const void* v_cache,
  * rounding decides, and from 2^31 on results may be NaN.  One kernel launch.
  * Limits: those of a2 and n5; num_pages*Hkv*page_size <= 2^32; scale and its product
  * with log2(e) positive and finite; flags: SS_STREAM_EXCLUDE_SELF only.
- * A sequence is cut into splits of equal length, chosen from its own length and
- * ss_msa_mx_plan's number of splits; no other sequence changes its result.
+ * A sequence is cut into splits of equal length, chosen from its own length, the call's
+ * shape and the format (at most ss_msa_mx_plan's number); no other sequence's length or
+ * contents change its result.
  * workspace: at least ss_msa_mx_workspace_bytes(...) bytes with max_seq_len =
  * max_pages_per_seq*page_size (not used if the plan has one split).  Its front holds
  * counters, under the rules of a2: zeros before the first call
@@ -743,7 +744,8 @@ int ss_kv_read_mx(const void* k_cache, const void* k_scale, const void* v_cache,
  * the same time.  One workspace can serve this call and a2 in turn.
  * ss_msa_mx_plan: most splits a sequence has in a call of this shape and query rows per
  * workgroup; either pointer may be NULL.  Host-only.  A max_seq_len above 2^30, the most
- * that a block table may hold, counts as 2^30.
+ * that a block table may hold, counts as 2^30.  Both queries answer for the format that
+ * needs more.
  */
 size_t ss_msa_mx_workspace_bytes(int B, int T, int gamma, int H, int Hkv, int D, int max_seq_len);
 int ss_msa_mx_plan(int B, int T, int gamma, int H, int Hkv, int D, int max_seq_len, int* n_splits,

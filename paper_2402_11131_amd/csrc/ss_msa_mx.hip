@@ -266,7 +266,17 @@ struct MxPlan {
   size_t part_o_at, part_lse_at, total_bytes;
 };
 
-static MxPlan mx_plan(int B, int R, int H, int Hkv, int D, int max_len) {
+// Workgroups of the kernel for few rows that the chip holds: two or three per compute unit.  Single tokens of heads of 128 in 8
+// bits, counted with three / with the two that fit, us: 256 items of 8192 tokens 102 / 92, 128 items 57 /
+// 50, 512 items of 4096 99 / 88, 1024 items 191 / 174; where that splits and the other count did not, 640 items 121 / 124, 768
+// items 130 / 139 (a last round that does not fill the chip goes faster than the rule counts).
+static int mx_resident(int tiles, int D, bool fp8) {
+  if (D == 128) return 256 * (tiles == 2 ? fp8 ? MxShape<128, true, 2>::WGS : MxShape<128, false, 2>::WGS
+                                         : fp8 ? MxShape<128, true, 1>::WGS : MxShape<128, false, 1>::WGS);
+  return 256 * (tiles == 2 ? fp8 ? MxShape<64, true, 2>::WGS : MxShape<64, false, 2>::WGS
+                           : fp8 ? MxShape<64, true, 1>::WGS : MxShape<64, false, 1>::WGS);
+}
+static MxPlan mx_plan(int B, int R, int H, int Hkv, int D, int max_len, bool fp8) {
   MxPlan p;
   const int F = (H / Hkv) * R, tiles = ceil_div(F, 16);
   int units, resident;  // waves of a workgroup that merge; workgroups that the chip holds
@@ -277,7 +287,7 @@ static MxPlan mx_plan(int B, int R, int H, int Hkv, int D, int max_len) {
     p.kernel = MxKernel{tiles, 1};
     p.n_qc = 1;
     units = kMxWaves;
-    resident = tiles == 1 ? 768 : 512;
+    resident = mx_resident(tiles, D, fp8);
   } else {
     // Up to five: a wave each, and two to four groups.  More: two per wave and as few chunks as there can be of up to eight (five
     // tiles that way: 51 us, 41 the other; four sequences of 4096 tokens, 32 heads).
@@ -332,14 +342,15 @@ extern "C" {
 size_t ss_msa_mx_workspace_bytes(int B, int T, int gamma, int H, int Hkv, int D, int max_seq_len) {
   ss::clear_error();
   if (ss::mx_check_shape("ss_msa_mx_workspace_bytes", B, T, gamma, H, Hkv, D) != SS_OK) return 0;
-  return ss::mx_plan(B, T * (1 + gamma), H, Hkv, D, max_seq_len).total_bytes;
+  return max(ss::mx_plan(B, T * (1 + gamma), H, Hkv, D, max_seq_len, false).total_bytes,
+             ss::mx_plan(B, T * (1 + gamma), H, Hkv, D, max_seq_len, true).total_bytes);
 }
 
 int ss_msa_mx_plan(int B, int T, int gamma, int H, int Hkv, int D, int max_seq_len, int* n_splits, int* rows_per_workgroup) {
   ss::clear_error();
   if (int rc = ss::mx_check_shape("ss_msa_mx_plan", B, T, gamma, H, Hkv, D)) return rc;
-  const ss::MxPlan p = ss::mx_plan(B, T * (1 + gamma), H, Hkv, D, max_seq_len);
-  if (n_splits) *n_splits = p.n_splits;
+  const ss::MxPlan p = ss::mx_plan(B, T * (1 + gamma), H, Hkv, D, max_seq_len, false);
+  if (n_splits) *n_splits = max(p.n_splits, ss::mx_plan(B, T * (1 + gamma), H, Hkv, D, max_seq_len, true).n_splits);
   if (rows_per_workgroup) *rows_per_workgroup = 16 * p.kernel.nt * p.kernel.nw;
   return SS_OK;
 }
@@ -362,7 +373,8 @@ int ss_msa_attention_mx(const void* q, const void* k_new, const void* v_new, con
   SS_REQUIRE((((uintptr_t)q | (uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)out) & 15) == 0, SS_ERR_INVALID_ARG,
              "%s: q, k_new, v_new or out not aligned to 16 bytes", fn);
   const int R = T * (1 + gamma);
-  const MxPlan plan = mx_plan(B, R, H, Hkv, D, max_pages_per_seq * page_size);
+  const bool fp8 = format == SS_KV_MXFP8;
+  const MxPlan plan = mx_plan(B, R, H, Hkv, D, max_pages_per_seq * page_size, fp8);
   SS_REQUIRE(plan.n_splits == 1 || (workspace != nullptr && workspace_bytes >= plan.total_bytes), SS_ERR_WORKSPACE,
              "%s: workspace of %zu bytes needed, %zu given", fn, plan.total_bytes, workspace_bytes);
   const long wgs = ((long)B * Hkv * plan.n_splits + 7) / 8 * 8 * plan.n_qc;
@@ -381,7 +393,6 @@ int ss_msa_attention_mx(const void* q, const void* k_new, const void* v_new, con
   a.scale_log2 = scale * 1.4426950408889634f;
   a.flags = flags;
   hipStream_t st = (hipStream_t)stream;
-  const bool fp8 = format == SS_KV_MXFP8;
   return plan.kernel.nw == 1 ? launch_msa_mx(a, plan.kernel, fp8, wgs, st) : launch_msa_mx_rows(a, plan.kernel, fp8, wgs, st);
 }
 
