@@ -269,7 +269,9 @@ struct MxPlan {
 // Workgroups of the kernel for few rows that the chip holds: two or three per compute unit.  Single tokens of heads of 128 in 8
 // bits, counted with three / with the two that fit, us: 256 items of 8192 tokens 102 / 92, 128 items 57 /
 // 50, 512 items of 4096 99 / 88, 1024 items 191 / 174; where that splits and the other count did not, 640 items 121 / 124, 768
-// items 130 / 139 (a last round that does not fill the chip goes faster than the rule counts).
+// items 130 / 139 (a last round that does not fill the chip goes faster than the rule counts).  Two tiles of heads of 64 in 4 bits
+// are counted with two per compute unit though three fit: 512 items of 4096 tokens 46 us, 50 with three, 1024 items 82 / 90, 640
+// items 61 / 57, 768 items 66 / 60.
 static int mx_resident(int tiles, int D, bool fp8) {
   if (D == 128) return 256 * (tiles == 2 ? fp8 ? MxShape<128, true, 2>::WGS : MxShape<128, false, 2>::WGS
                                          : fp8 ? MxShape<128, true, 1>::WGS : MxShape<128, false, 1>::WGS);
