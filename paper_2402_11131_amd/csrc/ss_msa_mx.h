@@ -33,18 +33,19 @@ struct MsaMxArgs {
   unsigned int* arrive;  // [items, U]: splits that have arrived; zero before the call, zero again after it
   int B, T, gamma, R, H, g, n_splits, n_qc;
   float scale_log2;
+  // Running maximum before the first score: below every score whose product with scale_log2 an fp32 number holds, and its own
+  // product with it is one too (rows that see nothing of a block keep it, and -inf * scale_log2 - (-inf) would be NaN).
+  float no_max;
   uint32_t flags;
 };
 
 constexpr float kMxLazyLog2 = 16.0f;
-// Running maximum before the first score: below every score whose product with c = scale * log2(e) an fp32 number holds, and its
-// own product with c is one too (rows that see nothing of a block keep it, and -inf * c - (-inf) would be NaN).
-SS_DEV float mx_no_maximum(float c) { return -3e38f / fmaxf(c, 1.f); }
 
 // Tokens per split of a sequence of L in a call that was planned with up to n_splits: a share of L, but no fewer than are worth
 // it.  One row, 8 KV heads: 128 tokens of a split take 1 us, merging two splits 2 us and each further one a quarter more, so the
-// least worthwhile length grows with the root of L.  (512 tokens: unsplit 8.7 us, halves 8.9; 1024: 12.6 and, in quarters, 9.1;
-// 4096: splits of 256 / 512 / 1024 / 2048 tokens 12.5 / 12.5 / 15.7 / 23 us.)
+// least worthwhile length grows with the root of L.  Two splits from 410 tokens on: few rows lose or gain little there, many rows
+// gain (512 tokens, unsplit / halves, us: one row 8.8 / 8.9, in 8 bits 9.3 / 9.0, heads of 64 7.4 / 7.7; 320 rows 22.9 / 20.3).
+// Later (one row): 1024 tokens 12.5 and, in quarters, 9.1; 4096 in splits of 256 / 512 / 1024 / 2048 tokens 12.5 / 12.5 / 15.7 / 23.
 SS_HD int mx_split_len(int L, int n_splits) {
   const float root = 5.f * sqrtf((float)L);
   const int least = root < 256.f ? 256 : (int)root & ~127;
@@ -356,7 +357,9 @@ struct MxReader {
   }
 };
 
-// Scores to probabilities, rounded to bf16; the sum takes the rounded ones.
+// Scores to probabilities, rounded to bf16; the sum takes the rounded ones.  The product with V takes bf16 operands.  A result's
+// error in the 2-norm grows from 1.6e-3 to 1.7e-3, which its own rounding to bf16 makes of it, to 1.8e-3 to 2.1e-3; probabilities in
+// two parts, which would leave it there, cost as many matrix instructions again as the values take, 8 of 12 per 16 rows and 32 keys.
 SS_DEV bf16x8 mx_softmax(const floatx4 (&S)[2], float c, float m_run, float& l_run) {
   const float nmc = -(m_run * c);
   uintx4 P;

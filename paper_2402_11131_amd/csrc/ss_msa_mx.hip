@@ -79,12 +79,12 @@ __global__ __launch_bounds__(64 * kMxWaves, (MxShape<D, FP8, NT>::WGS)) void msa
     }
   }
 
-  const float c = a.scale_log2, lazy_thr = kMxLazyLog2 / c, m_none = mx_no_maximum(c);
+  const float c = a.scale_log2, lazy_thr = kMxLazyLog2 / c;
   floatx4 O[NT][DT], S[NT][2];
   float m_run[NT], l_run[NT];  // maximum of the query row, sum of this lane's probabilities
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    m_run[t] = m_none;
+    m_run[t] = a.no_max;
     l_run[t] = 0.f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) O[t][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -393,6 +393,7 @@ int ss_msa_attention_mx(const void* q, const void* k_new, const void* v_new, con
   a.part_lse = (float*)(ws + plan.part_lse_at);
   a.B = B; a.T = T; a.gamma = gamma; a.R = R; a.H = H; a.g = H / Hkv; a.n_splits = plan.n_splits; a.n_qc = plan.n_qc;
   a.scale_log2 = scale * 1.4426950408889634f;
+  a.no_max = -3e38f / fmaxf(a.scale_log2, 1.f);
   a.flags = flags;
   hipStream_t st = (hipStream_t)stream;
   return plan.kernel.nw == 1 ? launch_msa_mx(a, plan.kernel, fp8, wgs, st) : launch_msa_mx_rows(a, plan.kernel, fp8, wgs, st);

@@ -98,12 +98,12 @@ __global__ __launch_bounds__(64 * NW * G, (MxRowsShape<D, FP8, NW, NT, G>::PER_S
       if (i < n_mine) issue(i, i);
   }
 
-  const float c = a.scale_log2, lazy_thr = kMxLazyLog2 / c, m_none = mx_no_maximum(c);
+  const float c = a.scale_log2, lazy_thr = kMxLazyLog2 / c;
   floatx4 O[NT][DT], S[NT][2];
   float m_run[NT], l_run[NT];  // maximum of the query row, sum of this lane's probabilities
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    m_run[t] = m_none;
+    m_run[t] = a.no_max;
     l_run[t] = 0.f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) O[t][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
