@@ -13,10 +13,11 @@
 // last to every barrier (NT = 2, eight of up to 32768 tokens, 640 rows: 1354 us, 1017 with quarters).  What a wave takes of a raw
 // block is read before the barrier and used behind it (939 us).
 //
-// Per 16 rows and 32 keys (D 128, 4 bits) 12 matrix instructions, 256 cycles of a SIMD, and 64 (NT = 1) or 49 (NT = 2) vector
-// instructions; 10 or 6 KB read from LDS.  NT = 2, eight sequences of 32768 tokens, 640 rows: 646 us, 1060 TFLOP/s; matrix pipe 43 %
-// and vector instructions 49 % of the cycles, which overlap little.  NT = 1, four of 4096, 32 heads, 80 rows: 40 us, 535 TFLOP/s;
-// 32 % and 44 %, 0.9 us from barrier to barrier: two to three waves per SIMD hide too little of each other's chain.
+// Per 16 rows and 32 keys (D 128, 4 bits) 12 matrix instructions, 256 cycles of a SIMD, and 62 (NT = 1) or 48 (NT = 2) vector
+// instructions; 10 or 6 KB read from LDS.  NT = 2, eight sequences of 32768 tokens, 640 rows: 637 us, 1080 TFLOP/s; in a run with
+// counters (685 us, 2.15 GHz) the matrix pipe is busy 45 % and vector instructions are active 51 % of the cycles, which overlap
+// little.  NT = 1, four of 4096, 32 heads, 80 rows: 40 us, 535 TFLOP/s; with counters (43.9 us, 2.03 GHz) 24 % and 40 %, and waves
+// wait a third of their time: ten waves lie on the four SIMDs as 3, 3, 2 and 2, and the barrier every 0.9 us waits for the threes.
 #include "ss_msa_mx.h"
 
 #include <mutex>
