@@ -50,7 +50,7 @@ SS_HD int mx_split_len(int L, int n_splits) {
   const float root = 5.f * sqrtf((float)L);
   const int least = root < 256.f ? 256 : (int)root & ~127;
   if (5 * (long)L < 8 * (long)least) n_splits = 1;
-  const int even = (L + n_splits - 1) / n_splits, up = (even + 127) & ~127;
+  const int even = (L - 1) / n_splits + 1, up = (even + 127) & ~127;  // (L + n_splits may pass 32 bits)
   return n_splits > 1 && up < least ? least : up < 128 ? 128 : up;
 }
 
@@ -358,7 +358,7 @@ struct MxReader {
 };
 
 // Scores to probabilities, rounded to bf16; the sum takes the rounded ones.  The product with V takes bf16 operands.  A result's
-// error in the 2-norm grows from 1.6e-3 to 1.7e-3, which its own rounding to bf16 makes of it, to 1.8e-3 to 2.1e-3; probabilities in
+// error in the 2-norm grows from 1.6e-3 to 1.7e-3, which its own rounding to bf16 makes of it, to 1.8e-3 to 2.3e-3; probabilities in
 // two parts, which would leave it there, cost as many matrix instructions again as the values take, 8 of 12 per 16 rows and 32 keys.
 SS_DEV bf16x8 mx_softmax(const floatx4 (&S)[2], float c, float m_run, float& l_run) {
   const float nmc = -(m_run * c);
